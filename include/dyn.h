@@ -28,7 +28,7 @@
  *     word at the start of the workspace, which dyn_workspace_status reads back.
  *   - Cells are numbered cell = w * G + g with w the window and g the class,
  *     g = (model * n_in_bin + in_bin) * n_out_bin + out_bin.
- *   - All floating point is IEEE binary64 without contraction.  Window and tick lengths,
+ *   - All floating point of the planner is IEEE binary64 without contraction.  Window and tick lengths,
  *     max_load_tps and the spacings of the load grid must lie in [1e-100, 1e100]
  *     (DYN_E_RANGE / DYN_E_NOTFINITE otherwise): inside that range every division of the
  *     method is reproduced exactly by the kernels' reciprocal-based form.
@@ -472,6 +472,128 @@ int dyn_hierarchy(dyn_profile* profile, const dyn_trace_view* coarse, const dyn_
                   const dyn_hierarchy_out* out, void* workspace, size_t workspace_bytes,
                   void* hip_stream);
 
+/* ---------------------------------------------------- the step that a profile is measured on --
+ * Section IV-A, "Generating LLM profiles": the tables above are measured by running a model's
+ * steps at the lengths and loads of the request classes.  What of a step depends on those lengths
+ * is the key/value cache and the attention that reads it; these entry points are that part, for
+ * steps that mix prompts (prefill: TTFT) and single tokens (generation: TBT) as a server does.
+ *
+ * The cache of one layer is k_cache and v_cache, each [n_page][n_kv_head][page_tokens][head_dim],
+ * contiguous and 16-byte aligned, in the queries' type or in 8 bits (DYN_T_E4M3, with a factor per
+ * key head).  Position x of request b lies in page block_table[b][x / page_tokens], row
+ * x % page_tokens; its slot is page * page_tokens + row.  The new tokens of all requests lie one
+ * request after the other: request b has tokens cu_new[b] .. cu_new[b+1]-1.
+ * Limits: page_tokens a power of two up to 4096, n_page * page_tokens < 2^31,
+ * n_req * max_pages < 2^31, n_q_head a multiple of n_kv_head, head_dim a multiple of 16 up to
+ * 128.  These calls need no profile handle; they may be captured into a HIP graph.        */
+#define DYN_T_F16 1
+#define DYN_T_BF16 2
+#define DYN_T_E4M3 3      /* 8-bit cache: 4 exponent bits, 3 fraction bits, no infinities, largest value 448 */
+#define DYN_WS_NO_PAGES 16u /* kv_step: a request found too few free pages, or has more tokens than its row of the table holds */
+#define DYN_WS_BAD_PAGE 32u /* a page number outside the cache, or a free list that is longer than the cache */
+
+/* One step's requests.  DEVICE arrays, caller-owned.
+ *   ctx_len    [n_req] tokens of the request that the cache holds, >= 0
+ *   new_len    [n_req] tokens that this step adds (1: generation, more: a chunk of a prompt, 0: none),
+ *              or DYN_KV_RELEASE: the request is through and its pages go back to the free list
+ *   block_table [n_req][max_pages], in and out: entries of the tokens in the cache must be valid,
+ *              the entries of new pages are written
+ *   free_pages [n_page], in and out: a ring; free_state[2] = {first, count}: the free pages are
+ *              free_pages[(first + i) % n_page], i < count                                  */
+#define DYN_KV_RELEASE (-1)
+typedef struct {
+  int32_t n_req, n_token;   /* requests (>= 1); new tokens: the sum of the positive new_len (>= 0) */
+  int32_t page_tokens, n_page, max_pages;
+  const int32_t* ctx_len; const int32_t* new_len;
+  int32_t* block_table; int32_t* free_pages; const int32_t* free_state;
+} dyn_kv_requests;
+typedef struct {          /* DEVICE, caller-owned; none may alias an input                   */
+  int32_t* cu_new;     /* [n_req+1] first new token of every request                        */
+  int32_t* kv_len;     /* [n_req] tokens its queries may see: ctx + new, 0 if refused or released */
+  int32_t* next_len;   /* [n_req] the next step's ctx_len: ctx + new, ctx if refused, 0 if released */
+  int32_t* pos;        /* [n_token] position, -1 if refused                                 */
+  int32_t* slot;       /* [n_token] slot, -1 if refused (or its page is not in the cache)   */
+  int32_t* free_state; /* [2]                                                               */
+} dyn_kv_plan;
+
+/* Block tables and slot maps from request lengths.  Pages are handed out in the order of the
+ * requests: a request whose pages, with those of all requests before it, are more than the free ones
+ * is refused (its tokens get position and slot -1, nothing of it is stored or seen, DYN_WS_NO_PAGES);
+ * requests that need no new page go on.  Released pages are handed out from the next step on.
+ * One launch up to 2048 requests, two beyond.  Lengths that cannot be (ctx_len < 0, new_len < -1, a
+ * sum that differs from n_token) raise DYN_WS_BAD_REQUEST.  Workspace DEVICE, 256-byte aligned,
+ * dyn_kv_step_workspace bytes.                                                            */
+size_t dyn_kv_step_workspace(int32_t n_req);
+int dyn_kv_step(const dyn_kv_requests* requests, const dyn_kv_plan* out, void* workspace, size_t workspace_bytes,
+                void* hip_stream);
+
+/* Rotary frequencies (HOST): inv_freq[i] = base^(-2i/rotary_dim), i < rotary_dim/2, in radians per
+ * position, for contexts stretched by `factor`: DYN_ROPE_LINEAR divides all by the factor;
+ * DYN_ROPE_PARTS divides those that make at most slow_turns turns over original_tokens
+ * positions, leaves those of fast_turns and more, and blends linearly in the turns between.
+ * *amplitude (may be NULL) receives 1, with DYN_ROPE_PARTS 0.1 ln(factor) + 1.               */
+#define DYN_ROPE_PLAIN 0
+#define DYN_ROPE_LINEAR 1
+#define DYN_ROPE_PARTS 2
+typedef struct {
+  int32_t rotary_dim;       /* even, 2 .. 128                                              */
+  int32_t scaling;          /* DYN_ROPE_*                                                  */
+  double base;              /* > 0                                                         */
+  double factor;            /* >= 1                                                        */
+  double original_tokens, slow_turns, fast_turns; /* DYN_ROPE_PARTS: > 0, slow < fast       */
+} dyn_rope_desc;
+int dyn_rope_frequencies(const dyn_rope_desc* desc, double* inv_freq, double* amplitude);
+
+/* [n_token][heads][head_dim], strides in elements, neighbouring elements of a head side by side. */
+typedef struct { void* data; int64_t token_stride, head_stride; } dyn_rows;
+
+/* Rotary positions and the new keys' and values' way into the cache: the first rotary_dim
+ * elements of every query and key head are turned by the angles pos * inv_freq[i] (pairs
+ * (i, i + rotary_dim/2), or with `interleaved` (2i, 2i+1)) and multiplied by `amplitude`; keys
+ * and values are stored in their slots, queries in q_out (which must not overlap q, k or v,
+ * nor the cache).  Angles in 64 bits, the products in 32, one rounding at the end.  In an 8-bit
+ * cache stored = value / scale, beyond +-448 +-448; NaN stays NaN.  A slot outside the cache
+ * (-1) is not stored.  Two tokens may not have the same slot.                              */
+typedef struct {
+  int32_t n_token, n_q_head, n_kv_head, head_dim;
+  int32_t type, cache_type;        /* DYN_T_F16 or DYN_T_BF16; the same or DYN_T_E4M3          */
+  int32_t page_tokens, n_page;
+  dyn_rows q, k, v, q_out;         /* DEVICE                                               */
+  const int32_t* pos; const int32_t* slot;     /* DEVICE [n_token], as dyn_kv_step returns them */
+  void* k_cache; void* v_cache;
+  const float* k_scale; const float* v_scale;  /* DEVICE [n_kv_head] or NULL = 1; 8-bit caches only */
+  int32_t rotary_dim, interleaved; /* even, 0 .. head_dim                                   */
+  const double* inv_freq;          /* HOST [rotary_dim/2], finite                           */
+  double amplitude;
+} dyn_append;
+int dyn_rope_append(const dyn_append* args, void* hip_stream);
+
+/* Attention of the new tokens over the cache.  Token i of request b's n new ones stands at
+ * p = kv_len[b] - n + i and sees the positions j <= p, with window > 0 only those with
+ * j > p - window or j < n_sink:  out = softmax(scale * q.k) v over them, zero where there is none.
+ * Query head h reads key head h / (n_q_head / n_kv_head).  Products of 16-bit values are summed in
+ * 32 bits, the softmax is in 32 bits, its weights are rounded to `type` for the second product.
+ * What keys and values a row does not see hold (NaN, infinities) does not reach it.
+ * max_new and max_kv bound every request's new tokens and kv_len (HOST; the launch is shaped by
+ * them: a kv_len beyond max_kv is right but slower, a request of more new tokens than max_new may be
+ * left out).  Rows of a request whose table names a page outside the cache are not valid and raise DYN_WS_BAD_PAGE.
+ * Workspace DEVICE, 256-byte aligned, dyn_paged_attention_workspace bytes; it must be zero before its
+ * first use and may be used again for any later call as it is left (not by two calls at a time).  Its status bits
+ * add up over the calls.                                                                  */
+typedef struct {
+  int32_t n_req, n_token, n_q_head, n_kv_head, head_dim;
+  int32_t type, cache_type, page_tokens, n_page, max_pages;
+  int32_t max_new, max_kv, window, n_sink;     /* window 0: all                             */
+  float scale;
+  dyn_rows q, out;                 /* DEVICE; out must not overlap an input                 */
+  const void* k_cache; const void* v_cache;
+  const float* k_scale; const float* v_scale;
+  const int32_t* block_table; const int32_t* cu_new; const int32_t* kv_len;   /* DEVICE      */
+} dyn_attention;
+size_t dyn_paged_attention_workspace(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim,
+                                     int32_t max_new, int32_t max_kv);
+int dyn_paged_attention(const dyn_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------------- kernel timing (optional) --
  * Measurement aid, not part of the method: when enabled, the library brackets each of its
  * kernels with a pair of HIP events recorded on the stream the kernel is launched on, so
@@ -488,7 +610,10 @@ int dyn_hierarchy(dyn_profile* profile, const dyn_trace_view* coarse, const dyn_
 #define DYN_K_MIXED_COMBINE 8 /* mixed pools: assignment of instances and shares          */
 #define DYN_K_PATH 9          /* selection with transition overheads                     */
 #define DYN_K_HIER 10         /* the four kernels of the controller hierarchy            */
-#define DYN_K_COUNT 11
+#define DYN_K_KV_STEP 11      /* block tables and slot maps                              */
+#define DYN_K_ROPE_APPEND 12  /* rotary positions, new keys and values into the cache    */
+#define DYN_K_ATTENTION 13    /* attention over the paged cache                          */
+#define DYN_K_COUNT 14
 /* on != 0: create the event pool (up to `max_launches` launches per kernel are recorded,
  * later ones are not) and start recording; on == 0: stop and destroy the pool.         */
 int dyn_timing_enable(int on, int32_t max_launches);

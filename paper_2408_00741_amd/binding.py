@@ -23,10 +23,17 @@ __all__ = ["DynError", "Profile", "dyn_profile_load", "dyn_profile_free", "dyn_t
            "DYN_WS_BAD_OFFSETS", "DYN_WS_BAD_REQUEST", "DYN_WS_TICK_RANK", "DYN_WS_SORT_ABANDONED", "dyn_eval_select_ticks",
            "dyn_eval_ticks_workspace", "DYN_K_TICK_TOP", "DYN_K_TICK_SPACE", "DYN_K_TICK_MERGE", "DYN_K_MIXED_TYPES", "DYN_K_MIXED_COMBINE",
            "MixedPlan", "dyn_mixed_workspace", "dyn_eval_select_mixed", "DYN_K_PATH", "dyn_select_path_workspace",
-           "dyn_select_path", "dyn_account_workspace", "dyn_account", "dyn_hierarchy_workspace", "dyn_hierarchy", "DYN_K_HIER", "DYN_TICK_LIMIT", "DYN_TICK_DEPTH"]
+           "dyn_select_path", "dyn_account_workspace", "dyn_account", "dyn_hierarchy_workspace", "dyn_hierarchy", "DYN_K_HIER", "DYN_TICK_LIMIT", "DYN_TICK_DEPTH",
+           "dyn_kv_step", "dyn_kv_step_workspace", "dyn_rope_frequencies", "dyn_rope_append", "dyn_paged_attention", "dyn_paged_attention_workspace",
+           "DYN_KV_RELEASE", "DYN_WS_NO_PAGES", "DYN_WS_BAD_PAGE", "DYN_T_F16", "DYN_T_BF16", "DYN_T_E4M3", "DYN_ROPE_PLAIN", "DYN_ROPE_LINEAR",
+           "DYN_ROPE_PARTS", "DYN_K_KV_STEP", "DYN_K_ROPE_APPEND", "DYN_K_ATTENTION"]
 
 DYN_F_FEASIBLE, DYN_F_OVERLOAD, DYN_F_TTFT, DYN_F_TBT, DYN_F_BUDGET, DYN_F_EMPTY = 1, 2, 4, 8, 16, 32
 DYN_WS_BAD_OFFSETS, DYN_WS_BAD_REQUEST, DYN_WS_TICK_RANK, DYN_WS_SORT_ABANDONED = 1, 2, 4, 8
+DYN_WS_NO_PAGES, DYN_WS_BAD_PAGE = 16, 32
+DYN_KV_RELEASE = -1
+DYN_T_F16, DYN_T_BF16, DYN_T_E4M3 = 1, 2, 3
+DYN_ROPE_PLAIN, DYN_ROPE_LINEAR, DYN_ROPE_PARTS = 0, 1, 2
 DYN_TICK_LIMIT, DYN_TICK_DEPTH = 64, 8192
 DYN_STATIC_WORKSPACE_BYTES = 16 << 20
 
@@ -114,6 +121,38 @@ class _HierarchyOut(C.Structure):
                 ("window_energy_j", _vp), ("window_infeasible", _vp), ("path_cost", _vp), ("keep", _vp)]
 
 
+class _KvRequests(C.Structure):
+    _fields_ = [("n_req", _i32), ("n_token", _i32), ("page_tokens", _i32), ("n_page", _i32), ("max_pages", _i32),
+                ("ctx_len", _vp), ("new_len", _vp), ("block_table", _vp), ("free_pages", _vp), ("free_state", _vp)]
+
+
+class _KvPlan(C.Structure):
+    _fields_ = [("cu_new", _vp), ("kv_len", _vp), ("next_len", _vp), ("pos", _vp), ("slot", _vp), ("free_state", _vp)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("rotary_dim", _i32), ("scaling", _i32), ("base", _f64), ("factor", _f64), ("original_tokens", _f64),
+                ("slow_turns", _f64), ("fast_turns", _f64)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", _vp), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class _Append(C.Structure):
+    _fields_ = [("n_token", _i32), ("n_q_head", _i32), ("n_kv_head", _i32), ("head_dim", _i32), ("type", _i32), ("cache_type", _i32),
+                ("page_tokens", _i32), ("n_page", _i32), ("q", _Rows), ("k", _Rows), ("v", _Rows), ("q_out", _Rows), ("pos", _vp),
+                ("slot", _vp), ("k_cache", _vp), ("v_cache", _vp), ("k_scale", _vp), ("v_scale", _vp), ("rotary_dim", _i32),
+                ("interleaved", _i32), ("inv_freq", _vp), ("amplitude", _f64)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("n_req", _i32), ("n_token", _i32), ("n_q_head", _i32), ("n_kv_head", _i32), ("head_dim", _i32), ("type", _i32),
+                ("cache_type", _i32), ("page_tokens", _i32), ("n_page", _i32), ("max_pages", _i32), ("max_new", _i32), ("max_kv", _i32),
+                ("window", _i32), ("n_sink", _i32), ("scale", C.c_float), ("q", _Rows), ("out", _Rows), ("k_cache", _vp), ("v_cache", _vp),
+                ("k_scale", _vp), ("v_scale", _vp), ("block_table", _vp), ("cu_new", _vp), ("kv_len", _vp)]
+
+
 _lib.dyn_last_error.restype = C.c_char_p
 _lib.dyn_profile_load.restype = C.c_int
 _lib.dyn_profile_load.argtypes = [C.POINTER(_ProfileDesc), _vp, C.POINTER(_vp)]
@@ -172,13 +211,26 @@ _lib.dyn_hierarchy_workspace.argtypes = [_i32, _i32, _i32, _i32]
 _lib.dyn_hierarchy.restype = C.c_int
 _lib.dyn_hierarchy.argtypes = [_vp, C.POINTER(_TraceView), C.POINTER(_TraceView), _i32, C.POINTER(_Controllers),
                                C.POINTER(_Objective), C.POINTER(_HierarchyOut), _vp, _sz, _vp]
+_lib.dyn_kv_step_workspace.restype = _sz
+_lib.dyn_kv_step_workspace.argtypes = [_i32]
+_lib.dyn_kv_step.restype = C.c_int
+_lib.dyn_kv_step.argtypes = [C.POINTER(_KvRequests), C.POINTER(_KvPlan), _vp, _sz, _vp]
+_lib.dyn_rope_frequencies.restype = C.c_int
+_lib.dyn_rope_frequencies.argtypes = [C.POINTER(_RopeDesc), _vp, C.POINTER(C.c_double)]
+_lib.dyn_rope_append.restype = C.c_int
+_lib.dyn_rope_append.argtypes = [C.POINTER(_Append), _vp]
+_lib.dyn_paged_attention_workspace.restype = _sz
+_lib.dyn_paged_attention_workspace.argtypes = [_i32] * 7
+_lib.dyn_paged_attention.restype = C.c_int
+_lib.dyn_paged_attention.argtypes = [C.POINTER(_Attention), _vp, _sz, _vp]
 _lib.dyn_timing_enable.restype = C.c_int
 _lib.dyn_timing_enable.argtypes = [C.c_int, _i32]
 _lib.dyn_timing_reset.restype = C.c_int
 _lib.dyn_timing_read.restype = C.c_int
 _lib.dyn_timing_read.argtypes = [_i32, C.POINTER(C.c_double), C.POINTER(_i64)]
 (DYN_K_CELL, DYN_K_SPACE, DYN_K_SELECT, DYN_K_TOTALS, DYN_K_TICK_TOP, DYN_K_TICK_SPACE, DYN_K_TICK_MERGE,
- DYN_K_MIXED_TYPES, DYN_K_MIXED_COMBINE, DYN_K_PATH, DYN_K_HIER) = range(11)
+ DYN_K_MIXED_TYPES, DYN_K_MIXED_COMBINE, DYN_K_PATH, DYN_K_HIER, DYN_K_KV_STEP,
+ DYN_K_ROPE_APPEND, DYN_K_ATTENTION) = range(14)
 
 
 def dyn_timing_enable(on: bool, max_launches: int = 4096):
@@ -685,4 +737,135 @@ def dyn_select_config(profile: Profile, space: Dict[str, torch.Tensor], n_window
     se = _selection_struct(out)
     _check(_lib.dyn_select_config(profile.handle, C.byref(sp), plan.cfg, K, C.byref(plan.obj), n_window,
                                   float(window_s), C.byref(se), _stream(stream)), "dyn_select_config")
+    return out
+
+
+# ---- the serving step that a profile is measured on ------------------------------------------------------------
+
+_TYPES = {torch.float16: DYN_T_F16, torch.bfloat16: DYN_T_BF16, torch.float8_e4m3fn: DYN_T_E4M3}
+
+
+def _type(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be float16, bfloat16 or (a cache) float8_e4m3fn, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype) -> _Rows:
+    """[n_token][heads][head_dim] with neighbouring elements of a head side by side; any other strides."""
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or t.stride(2) != 1:
+        raise ValueError(f"{name} must be a GPU tensor of {dtype} and shape {tuple(shape)} whose last dimension is contiguous")
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _scale(t: Optional[torch.Tensor], n: int, name: str):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have one factor per key head")
+    return _dp(t, torch.float32, name)
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor):
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("k_cache and v_cache must be alike, [n_page][n_kv_head][page_tokens][head_dim]")
+    return _dp(k_cache, None, "k_cache"), _dp(v_cache, None, "v_cache"), _type(k_cache, "k_cache")
+
+
+def dyn_kv_step_workspace(n_req: int) -> int:
+    return int(_lib.dyn_kv_step_workspace(n_req))
+
+
+def dyn_kv_step(ctx_len: torch.Tensor, new_len: torch.Tensor, n_token: int, block_table: torch.Tensor, free_pages: torch.Tensor,
+                free_state: torch.Tensor, page_tokens: int, workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Block tables and slot maps of a step.  block_table and free_pages are updated in place; returns cu_new, kv_len, next_len, pos,
+    slot, free_state (and the two updated tensors) and the workspace, whose status dyn_workspace_status reads."""
+    B, dev = ctx_len.numel(), ctx_len.device
+    if new_len.numel() != B or block_table.dim() != 2 or block_table.shape[0] != B or free_state.numel() != 2:
+        raise ValueError("ctx_len, new_len [n_req], block_table [n_req][max_pages] and free_state [2] do not fit together")
+    i32 = torch.int32
+    r = _KvRequests(B, n_token, page_tokens, free_pages.numel(), block_table.shape[1], _dp(ctx_len, i32, "ctx_len"), _dp(new_len, i32, "new_len"),
+                    _dp(block_table, i32, "block_table"), _dp(free_pages, i32, "free_pages"), _dp(free_state, i32, "free_state"))
+    need = dyn_kv_step_workspace(B)
+    # one allocation for what is returned and the workspace, each part 256-byte aligned
+    sizes = (B + 1, B, B, n_token, n_token, 2)
+    up = [(4 * n + 255) // 256 * 256 for n in sizes]
+    own = need if workspace is None else 0
+    base = torch.empty(own + sum(up), dtype=torch.uint8, device=dev)
+    words, at, out = base.view(i32), own // 4, []
+    for n, u in zip(sizes, up):
+        out.append(words[at:at + n])
+        at += u // 4
+    if workspace is None:
+        workspace = base[:own]
+    p = base.data_ptr() + own
+    ptr = []
+    for u in up:
+        ptr.append(p)
+        p += u
+    plan = _KvPlan(*ptr)
+    _check(_lib.dyn_kv_step(C.byref(r), C.byref(plan), _dp(workspace), workspace.numel(), _stream(stream)), "dyn_kv_step")
+    return {"cu_new": out[0], "kv_len": out[1], "next_len": out[2], "pos": out[3], "slot": out[4], "block_table": block_table,
+            "free_pages": free_pages, "free_state": out[5], "workspace": workspace}
+
+
+def dyn_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = DYN_ROPE_PLAIN, factor: float = 1.0, original_tokens: float = 0.0,
+                         slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """(inv_freq as a float64 array, amplitude) for dyn_rope_append."""
+    d = _RopeDesc(rotary_dim, scaling, base, factor, original_tokens, slow_turns, fast_turns)
+    w, amp = np.empty(max(rotary_dim // 2, 1), np.float64), C.c_double(1.0)
+    _check(_lib.dyn_rope_frequencies(C.byref(d), _hp(w), C.byref(amp)), "dyn_rope_frequencies")
+    return w, amp.value
+
+
+def dyn_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor,
+                    v_cache: torch.Tensor, inv_freq, interleaved: bool = False, rope_scale: float = 1.0, k_scale: Optional[torch.Tensor] = None,
+                    v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Turns queries and keys by their positions, stores keys and values in their slots; returns the queries.
+    q [n_token][n_q_head][head_dim], k and v [n_token][n_kv_head][head_dim] (views of one product's output will do)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [n_token][n_q_head][head_dim]")
+    T, H, D = q.shape
+    kc, vc, ct = _cache(k_cache, v_cache)
+    N, G, P, Dc = k_cache.shape
+    if Dc != D or pos.numel() != T or slot.numel() != T:
+        raise ValueError("queries, cache, pos and slot do not fit together")
+    w = _host(inv_freq, np.float64)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+    a = _Append(T, H, G, D, _type(q, "q"), ct, P, N, _rows(q, "q", q.shape, q.dtype), _rows(k, "k", (T, G, D), q.dtype),
+                _rows(v, "v", (T, G, D), q.dtype), _rows(out, "out", (T, H, D), q.dtype), _dp(pos, torch.int32, "pos"),
+                _dp(slot, torch.int32, "slot"), kc, vc, _scale(k_scale, G, "k_scale"), _scale(v_scale, G, "v_scale"), 2 * w.size,
+                int(interleaved), _hp(w), rope_scale)
+    _check(_lib.dyn_rope_append(C.byref(a), _stream(stream)), "dyn_rope_append")
+    return out
+
+
+def dyn_paged_attention_workspace(n_req: int, n_token: int, n_q_head: int, n_kv_head: int, head_dim: int, max_new: int, max_kv: int) -> int:
+    return int(_lib.dyn_paged_attention_workspace(n_req, n_token, n_q_head, n_kv_head, head_dim, max_new, max_kv))
+
+
+def dyn_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, cu_new: torch.Tensor,
+                        kv_len: torch.Tensor, max_new: int, max_kv: int, scale: Optional[float] = None, window: int = 0, n_sink: int = 0,
+                        k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of every request's new tokens over its pages; returns [n_token][n_q_head][head_dim].  max_new and max_kv: at least the
+    greatest number of new tokens and the greatest kv_len (max_new is n_token, max_kv what the table holds, where the caller does not know better).
+    scale: 1 / sqrt(head_dim) by default.  A caller that keeps a workspace (dyn_paged_attention_workspace bytes, zero when it is made) saves an
+    allocation and a fill per call."""
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q must be [n_token][n_q_head][head_dim], block_table [n_req][max_pages]")
+    T, H, D = q.shape
+    kc, vc, ct = _cache(k_cache, v_cache)
+    N, G, P, Dc = k_cache.shape
+    B = block_table.shape[0]
+    if Dc != D or cu_new.numel() != B + 1 or kv_len.numel() != B:
+        raise ValueError("queries, cache, block_table, cu_new and kv_len do not fit together")
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = torch.zeros(max(256, dyn_paged_attention_workspace(B, T, H, G, D, max_new, max_kv)), dtype=torch.uint8, device=q.device)
+    a = _Attention(B, T, H, G, D, _type(q, "q"), ct, P, N, block_table.shape[1], max_new, max_kv, window, n_sink,
+                   D ** -0.5 if scale is None else scale, _rows(q, "q", q.shape, q.dtype), _rows(out, "out", (T, H, D), q.dtype), kc, vc,
+                   _scale(k_scale, G, "k_scale"), _scale(v_scale, G, "v_scale"), _dp(block_table, torch.int32, "block_table"),
+                   _dp(cu_new, torch.int32, "cu_new"), _dp(kv_len, torch.int32, "kv_len"))
+    _check(_lib.dyn_paged_attention(C.byref(a), _dp(workspace), workspace.numel(), _stream(stream)), "dyn_paged_attention")
     return out

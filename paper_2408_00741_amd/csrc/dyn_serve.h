@@ -1,0 +1,54 @@
+// Internal declarations of the serving step's operators (not part of the ABI).
+#ifndef DYN_SERVE_H_
+#define DYN_SERVE_H_
+
+#include "dyn_internal.h"
+
+struct KvStepArgs {
+  const int32_t* ctx_len; const int32_t* new_len; int32_t n_req, n_token;
+  int32_t page_shift, n_page, max_pages;
+  int32_t* table; int32_t* ring; const int32_t* state;
+  int32_t* cu; int32_t* kv_len; int32_t* next_len; int32_t* pos; int32_t* slot; int32_t* state_out;
+  int32_t* need; int32_t* back;   // workspace [n_req + 1] each, sums over the requests before; not used by the one-launch form
+  WsHeader* header;
+};
+hipError_t dyn_launch_kv_step(const KvStepArgs& a, hipStream_t s);
+#define DYN_KV_ONE_LAUNCH 2048    // requests whose sums every block makes for itself
+
+#define DYN_ROPE_MAX_PAIRS 64     // head_dim / 2 at most: the frequencies travel in the kernel's arguments
+struct RopeArgs {
+  const void* q; const void* k; const void* v; void* q_out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in elements
+  const int32_t* pos; const int32_t* slot;
+  void* k_cache; void* v_cache; const float* k_scale; const float* v_scale;
+  int32_t n_token, n_q_head, n_kv_head, head_dim, page_shift, n_slot;
+  int32_t rotary, interleaved;
+  float amplitude;
+  int32_t type, cache_type, vec;  // vec: elements of one load
+  double turn[DYN_ROPE_MAX_PAIRS];   // turns (of 2 pi) per position
+};
+hipError_t dyn_launch_rope_append(const RopeArgs& a, hipStream_t s);
+
+struct AttnArgs {
+  const void* q; void* out; int64_t q_token, q_head, o_token, o_head;
+  const void* k_cache; const void* v_cache; const float* k_scale; const float* v_scale;
+  const int32_t* table; const int32_t* cu; const int32_t* kv_len;
+  int32_t n_req, n_token, n_kv_head, group, head_dim, page_shift, n_page, max_pages, window, n_sink;
+  float scale;
+  int32_t type, cache_type;
+  bool q_vec, o_vec;              // 16-byte loads of queries, 8-byte stores of outputs are aligned
+  int32_t max_new;
+  // the key axis is cut in at most n_chunk pieces of `tiles` tiles (narrow: requests of few rows, wide: the others)
+  int32_t n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide;
+  int32_t n_tile_wide;            // row tiles of the wide kernel at most, 0: none
+  float* part; float* part_ml;    // workspace: [chunk][token][head][head_dim] and [chunk][token][head][2]
+  uint32_t* arrived_narrow; uint32_t* arrived_wide;   // zero between calls
+  WsHeader* header;
+};
+hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s);
+#define DYN_ATTN_ROWS 32          // rows (new tokens x query heads of a key head) of one wave; requests of at most as many take the narrow kernel
+#define DYN_ATTN_KEYS_NARROW 32   // keys of a tile
+#define DYN_ATTN_KEYS_WIDE 64
+#define DYN_ATTN_WAVES_WIDE 4     // waves of a block of the wide kernel, each with rows of its own
+
+#endif  // DYN_SERVE_H_

@@ -1,0 +1,212 @@
+// C ABI of the serving step's operators: argument checks, the shapes of the launches, workspaces.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "dyn_serve.h"
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+bool hip_ok(hipError_t e, const char* what) {
+  if (e == hipSuccess) return true;
+  dyn_set_error("%s: %s", what, hipGetErrorString(e));
+  return false;
+}
+
+int page_shift_of(int32_t page_tokens) {   // -1: not a power of two in [1, 4096]
+  for (int s = 0; s <= 12; ++s)
+    if (page_tokens == 1 << s) return s;
+  return -1;
+}
+
+// What a cache and its heads may be.
+int check_cache(int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t type, int32_t cache_type, int32_t page_tokens, int32_t n_page) {
+  if (n_q_head < 1 || n_kv_head < 1 || n_q_head % n_kv_head || n_q_head > 65536) { dyn_set_error("n_q_head=%d must be a multiple of n_kv_head=%d, both in [1, 65536]", n_q_head, n_kv_head); return DYN_E_SHAPE; }
+  if (head_dim < 16 || head_dim > 128 || head_dim % 16) { dyn_set_error("head_dim=%d must be a multiple of 16 in [16, 128]", head_dim); return DYN_E_SHAPE; }
+  if (type != DYN_T_F16 && type != DYN_T_BF16) { dyn_set_error("type must be DYN_T_F16 or DYN_T_BF16"); return DYN_E_RANGE; }
+  if (cache_type != type && cache_type != DYN_T_E4M3) { dyn_set_error("cache_type must be the queries' type or DYN_T_E4M3"); return DYN_E_RANGE; }
+  if (page_shift_of(page_tokens) < 0) { dyn_set_error("page_tokens=%d must be a power of two up to 4096", page_tokens); return DYN_E_SHAPE; }
+  if (n_page < 1 || ((int64_t)n_page << page_shift_of(page_tokens)) >= ((int64_t)1 << 31)) { dyn_set_error("n_page < 1 or n_page * page_tokens >= 2^31"); return DYN_E_SHAPE; }
+  return DYN_OK;
+}
+
+bool aligned_rows(const dyn_rows& r, int elements) {   // elements of 2 bytes
+  return ((uintptr_t)r.data % (2 * elements)) == 0 && r.token_stride % elements == 0 && r.head_stride % elements == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dyn_kv_step_workspace(int32_t n_req) {
+  if (n_req < 1) return 0;
+  return 256 + 2 * align256(((size_t)n_req + 1) * sizeof(int32_t));
+}
+
+int dyn_kv_step(const dyn_kv_requests* r, const dyn_kv_plan* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!r || !out || !workspace) { dyn_set_error("requests, out or workspace is NULL"); return DYN_E_NULL; }
+  if (!r->ctx_len || !r->new_len || !r->block_table || !r->free_pages || !r->free_state || !out->cu_new || !out->kv_len || !out->next_len || !out->free_state) { dyn_set_error("an array is NULL"); return DYN_E_NULL; }
+  if (r->n_req < 1 || r->n_token < 0 || r->max_pages < 1) { dyn_set_error("n_req or max_pages < 1 or n_token < 0"); return DYN_E_SHAPE; }
+  if (r->n_token > 0 && (!out->pos || !out->slot)) { dyn_set_error("pos or slot is NULL"); return DYN_E_NULL; }
+  if ((int64_t)r->n_req * r->max_pages >= ((int64_t)1 << 31)) { dyn_set_error("n_req * max_pages must stay below 2^31"); return DYN_E_SHAPE; }
+  const int shift = page_shift_of(r->page_tokens);
+  if (shift < 0) { dyn_set_error("page_tokens=%d must be a power of two up to 4096", r->page_tokens); return DYN_E_SHAPE; }
+  if (r->n_page < 1 || ((int64_t)r->n_page << shift) >= ((int64_t)1 << 31)) { dyn_set_error("n_page < 1 or n_page * page_tokens >= 2^31"); return DYN_E_SHAPE; }
+  if (((int64_t)r->max_pages << shift) >= ((int64_t)1 << 31)) { dyn_set_error("max_pages * page_tokens must stay below 2^31"); return DYN_E_SHAPE; }
+  if (out->free_state == r->free_state || out->next_len == r->ctx_len || out->kv_len == r->ctx_len) { dyn_set_error("an output is an input"); return DYN_E_RANGE; }
+  const size_t per = align256(((size_t)r->n_req + 1) * sizeof(int32_t));
+  if (((uintptr_t)workspace & 255) || workspace_bytes < 256 + 2 * per) { dyn_set_error("workspace misaligned or too small"); return DYN_E_WORKSPACE; }
+  KvStepArgs a;
+  a.ctx_len = r->ctx_len; a.new_len = r->new_len; a.n_req = r->n_req; a.n_token = r->n_token;
+  a.page_shift = shift; a.n_page = r->n_page; a.max_pages = r->max_pages;
+  a.table = r->block_table; a.ring = r->free_pages; a.state = r->free_state;
+  a.cu = out->cu_new; a.kv_len = out->kv_len; a.next_len = out->next_len; a.pos = out->pos; a.slot = out->slot; a.state_out = out->free_state;
+  a.need = (int32_t*)((char*)workspace + 256); a.back = (int32_t*)((char*)workspace + 256 + per);
+  a.header = (WsHeader*)workspace;
+  return hip_ok(dyn_launch_kv_step(a, (hipStream_t)hip_stream), "kv step launch") ? DYN_OK : DYN_E_DEVICE;
+}
+
+int dyn_rope_frequencies(const dyn_rope_desc* d, double* inv_freq, double* amplitude) {
+  if (!d || !inv_freq) { dyn_set_error("desc or inv_freq is NULL"); return DYN_E_NULL; }
+  if (d->rotary_dim < 2 || d->rotary_dim > 2 * DYN_ROPE_MAX_PAIRS || d->rotary_dim % 2) { dyn_set_error("rotary_dim=%d must be even, 2 .. %d", d->rotary_dim, 2 * DYN_ROPE_MAX_PAIRS); return DYN_E_SHAPE; }
+  if (d->scaling < DYN_ROPE_PLAIN || d->scaling > DYN_ROPE_PARTS) { dyn_set_error("unknown scaling %d", d->scaling); return DYN_E_RANGE; }
+  if (!(d->base > 0.0) || !isfinite(d->base)) { dyn_set_error("base must be finite and > 0"); return DYN_E_RANGE; }
+  if (d->scaling != DYN_ROPE_PLAIN && (!(d->factor >= 1.0) || !isfinite(d->factor))) { dyn_set_error("factor must be finite and >= 1"); return DYN_E_RANGE; }
+  if (d->scaling == DYN_ROPE_PARTS && (!(d->original_tokens > 0.0) || !isfinite(d->original_tokens) || !(d->slow_turns >= 0.0) || !(d->fast_turns > d->slow_turns) || !isfinite(d->fast_turns))) { dyn_set_error("original_tokens must be > 0 and 0 <= slow_turns < fast_turns"); return DYN_E_RANGE; }
+  for (int i = 0; i < d->rotary_dim / 2; ++i) {
+    double w = pow(d->base, -2.0 * i / d->rotary_dim);
+    if (d->scaling == DYN_ROPE_LINEAR) w /= d->factor;
+    if (d->scaling == DYN_ROPE_PARTS) {
+      const double turns = d->original_tokens * w / 6.283185307179586;
+      const double fast = std::min(std::max((turns - d->slow_turns) / (d->fast_turns - d->slow_turns), 0.0), 1.0);
+      w = w / d->factor * (1.0 - fast) + w * fast;
+    }
+    inv_freq[i] = w;
+  }
+  if (amplitude) *amplitude = d->scaling == DYN_ROPE_PARTS ? 0.1 * log(d->factor) + 1.0 : 1.0;
+  return DYN_OK;
+}
+
+int dyn_rope_append(const dyn_append* p, void* hip_stream) {
+  if (!p) { dyn_set_error("args is NULL"); return DYN_E_NULL; }
+  if (p->n_token < 0) { dyn_set_error("n_token < 0"); return DYN_E_SHAPE; }
+  int rc = check_cache(p->n_q_head, p->n_kv_head, p->head_dim, p->type, p->cache_type, p->page_tokens, p->n_page);
+  if (rc) return rc;
+  if (p->rotary_dim < 0 || p->rotary_dim % 2 || p->rotary_dim > p->head_dim) { dyn_set_error("rotary_dim=%d must be even, 0 .. head_dim", p->rotary_dim); return DYN_E_SHAPE; }
+  if (p->rotary_dim && !p->inv_freq) { dyn_set_error("inv_freq is NULL"); return DYN_E_NULL; }
+  for (int i = 0; i < p->rotary_dim / 2; ++i)
+    if (!isfinite(p->inv_freq[i])) { dyn_set_error("inv_freq[%d] is not finite", i); return DYN_E_NOTFINITE; }
+  if (!isfinite(p->amplitude)) { dyn_set_error("amplitude is not finite"); return DYN_E_NOTFINITE; }
+  if ((p->k_scale || p->v_scale) && p->cache_type != DYN_T_E4M3) { dyn_set_error("scales belong to an 8-bit cache"); return DYN_E_RANGE; }
+  if (p->n_token == 0) return DYN_OK;
+  if (!p->q.data || !p->k.data || !p->v.data || !p->q_out.data || !p->pos || !p->slot || !p->k_cache || !p->v_cache) { dyn_set_error("an array is NULL"); return DYN_E_NULL; }
+  if ((uintptr_t)p->k_cache % 16 || (uintptr_t)p->v_cache % 16) { dyn_set_error("the cache must be 16-byte aligned"); return DYN_E_SHAPE; }
+  RopeArgs a;
+  a.q = p->q.data; a.k = p->k.data; a.v = p->v.data; a.q_out = p->q_out.data;
+  a.q_token = p->q.token_stride; a.q_head = p->q.head_stride; a.k_token = p->k.token_stride; a.k_head = p->k.head_stride;
+  a.v_token = p->v.token_stride; a.v_head = p->v.head_stride; a.o_token = p->q_out.token_stride; a.o_head = p->q_out.head_stride;
+  a.pos = p->pos; a.slot = p->slot; a.k_cache = p->k_cache; a.v_cache = p->v_cache; a.k_scale = p->k_scale; a.v_scale = p->v_scale;
+  a.n_token = p->n_token; a.n_q_head = p->n_q_head; a.n_kv_head = p->n_kv_head; a.head_dim = p->head_dim;
+  a.page_shift = page_shift_of(p->page_tokens); a.n_slot = p->n_page << a.page_shift;
+  a.rotary = p->rotary_dim; a.interleaved = p->interleaved != 0; a.amplitude = (float)p->amplitude;
+  a.type = p->type; a.cache_type = p->cache_type;
+  // elements of a load: as many as divide half the rotated part and as pointers and strides are aligned to
+  a.vec = 1;
+  for (int v : {8, 4})
+    if (a.vec == 1 && (p->rotary_dim / 2) % v == 0 && aligned_rows(p->q, v) && aligned_rows(p->k, v) && aligned_rows(p->v, v) && aligned_rows(p->q_out, v)) a.vec = v;
+  for (int i = 0; i < DYN_ROPE_MAX_PAIRS; ++i) a.turn[i] = i < p->rotary_dim / 2 ? p->inv_freq[i] / 6.283185307179586476925 : 0.0;
+  return hip_ok(dyn_launch_rope_append(a, (hipStream_t)hip_stream), "rope append launch") ? DYN_OK : DYN_E_DEVICE;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The pieces that the key axis is cut into, for the narrow and the wide kernel, and the places in the workspace.
+struct AttnShape {
+  int32_t n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
+  size_t ml, part, total;
+};
+constexpr int64_t kCounters = 16384;         // words of arrivals; launches that would need more are not cut
+constexpr size_t kPartBytes = 64u << 20;     // pieces' sums at most
+
+AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t max_new, int32_t max_kv, int32_t window,
+                          int32_t n_sink) {
+  AttnShape s;
+  const int64_t group = n_q_head / n_kv_head, rows = (int64_t)std::min(max_new, n_token) * group;
+  const int64_t seen = window > 0 ? std::min<int64_t>(max_kv, (int64_t)window + max_new + n_sink + 2 * DYN_ATTN_KEYS_WIDE) : max_kv;
+  const int64_t row_bytes = (int64_t)n_token * n_q_head * (head_dim + 2) * 4;
+  int64_t chunks = 1;
+  auto cut = [&](int64_t blocks, int64_t want, int64_t tiles, int64_t least, int64_t step, int32_t* n, int32_t* each) {   // at most n pieces of `each` tiles
+    int64_t c = blocks >= want ? 1 : (want + blocks - 1) / blocks;
+    c = std::min(c, std::max<int64_t>(1, tiles / least));
+    c = std::min<int64_t>(c, std::max<int64_t>(1, (int64_t)kPartBytes / std::max<int64_t>(row_bytes, 1)));
+    int64_t e = (tiles + c - 1) / c;
+    e = std::max<int64_t>(1, (e + step - 1) / step * step);
+    *n = (int32_t)std::max<int64_t>(1, (tiles + e - 1) / e);
+    *each = (int32_t)e;
+    chunks = std::max(chunks, c);   // the workspace holds as many as were wanted: never fewer for more keys
+  };
+  const int64_t narrow = (int64_t)n_req * n_kv_head;
+  cut(narrow, narrow <= kCounters / 2 ? 1024 : 1, (seen + DYN_ATTN_KEYS_NARROW - 1) / DYN_ATTN_KEYS_NARROW, 4, 4, &s.n_chunk_narrow, &s.tiles_narrow);
+  s.n_tile_wide = 0;
+  s.n_chunk_wide = s.tiles_wide = 1;
+  if (rows > DYN_ATTN_ROWS) {
+    const int64_t R = 32 * DYN_ATTN_WAVES_WIDE, all = (int64_t)n_token * group;
+    s.n_tile_wide = (int32_t)(all / R + n_req);
+    const int64_t blocks = std::max<int64_t>(1, all / R) * n_kv_head;
+    cut(blocks, (int64_t)s.n_tile_wide * n_kv_head <= kCounters / 2 ? 512 : 1, (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE, 4, 1, &s.n_chunk_wide, &s.tiles_wide);
+  }
+  s.ml = 256 + kCounters * sizeof(uint32_t);
+  s.part = s.ml + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * 2 * sizeof(float)) : 0);
+  s.total = s.part + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * head_dim * sizeof(float)) : 0);
+  return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dyn_paged_attention_workspace(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t max_new, int32_t max_kv) {
+  if (n_req < 1 || n_token < 0 || n_q_head < 1 || n_kv_head < 1 || n_q_head % n_kv_head || head_dim < 1 || max_new < 0 || max_kv < 0) return 0;
+  return attention_shape(n_req, n_token, n_q_head, n_kv_head, head_dim, max_new, max_kv, 0, 0).total;
+}
+
+int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!p || !workspace) { dyn_set_error("args or workspace is NULL"); return DYN_E_NULL; }
+  if (p->n_req < 1 || p->n_token < 0 || p->max_pages < 1 || p->max_new < 0 || p->max_kv < 0) { dyn_set_error("n_req or max_pages < 1, or n_token, max_new or max_kv < 0"); return DYN_E_SHAPE; }
+  int rc = check_cache(p->n_q_head, p->n_kv_head, p->head_dim, p->type, p->cache_type, p->page_tokens, p->n_page);
+  if (rc) return rc;
+  const int shift = page_shift_of(p->page_tokens);
+  if ((int64_t)p->n_req * p->max_pages >= ((int64_t)1 << 31) || ((int64_t)p->max_pages << shift) >= ((int64_t)1 << 31)) { dyn_set_error("n_req * max_pages and max_pages * page_tokens must stay below 2^31"); return DYN_E_SHAPE; }
+  const int64_t group = p->n_q_head / p->n_kv_head;
+  if ((int64_t)p->n_token * group >= ((int64_t)1 << 31) || ((int64_t)p->n_token * group / (32 * DYN_ATTN_WAVES_WIDE) + p->n_req) * p->n_kv_head >= ((int64_t)1 << 31)) { dyn_set_error("too many rows"); return DYN_E_SHAPE; }
+  if (p->window < 0 || p->n_sink < 0) { dyn_set_error("window or n_sink < 0"); return DYN_E_RANGE; }
+  if (!isfinite(p->scale)) { dyn_set_error("scale is not finite"); return DYN_E_NOTFINITE; }
+  if ((p->k_scale || p->v_scale) && p->cache_type != DYN_T_E4M3) { dyn_set_error("scales belong to an 8-bit cache"); return DYN_E_RANGE; }
+  if (p->n_token == 0) return DYN_OK;
+  if (!p->q.data || !p->out.data || !p->k_cache || !p->v_cache || !p->block_table || !p->cu_new || !p->kv_len) { dyn_set_error("an array is NULL"); return DYN_E_NULL; }
+  if ((uintptr_t)p->k_cache % 16 || (uintptr_t)p->v_cache % 16) { dyn_set_error("the cache must be 16-byte aligned"); return DYN_E_SHAPE; }
+  const int32_t max_kv = (int32_t)std::min<int64_t>(p->max_kv, (int64_t)p->max_pages << shift);
+  const AttnShape s = attention_shape(p->n_req, p->n_token, p->n_q_head, p->n_kv_head, p->head_dim, p->max_new, max_kv, p->window, p->n_sink);
+  if (((uintptr_t)workspace & 255) || workspace_bytes < s.total) { dyn_set_error("workspace misaligned or too small"); return DYN_E_WORKSPACE; }
+  AttnArgs a;
+  a.q = p->q.data; a.out = p->out.data; a.q_token = p->q.token_stride; a.q_head = p->q.head_stride; a.o_token = p->out.token_stride; a.o_head = p->out.head_stride;
+  a.k_cache = p->k_cache; a.v_cache = p->v_cache; a.k_scale = p->k_scale; a.v_scale = p->v_scale;
+  a.table = p->block_table; a.cu = p->cu_new; a.kv_len = p->kv_len;
+  a.n_req = p->n_req; a.n_token = p->n_token; a.n_kv_head = p->n_kv_head; a.group = (int32_t)group; a.head_dim = p->head_dim;
+  a.page_shift = shift; a.n_page = p->n_page; a.max_pages = p->max_pages; a.window = p->window; a.n_sink = p->n_sink;
+  a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
+  a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.max_new = p->max_new;
+  a.n_chunk_narrow = s.n_chunk_narrow; a.tiles_narrow = s.tiles_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;
+  char* base = (char*)workspace;
+  a.header = (WsHeader*)base;
+  a.arrived_narrow = (uint32_t*)(base + 256); a.arrived_wide = a.arrived_narrow + kCounters / 2;
+  a.part_ml = (float*)(base + s.ml); a.part = (float*)(base + s.part);
+  return hip_ok(dyn_launch_paged_attention(a, (hipStream_t)hip_stream), "attention launch") ? DYN_OK : DYN_E_DEVICE;
+}
+
+}  // extern "C"
