@@ -1,0 +1,225 @@
+// Device-side parts shared by the two attention kernels and the kernel that joins their pieces.
+//
+// Row (token i of request b, query head h) stands at p = kv_len - n + i and sees the keys j <= p with j > p - window or j < n_sink:
+//   o = sum_j exp(c q.k_j - m) v_j / sum_j exp(c q.k_j - m),   c = scale x the key head's scale,
+// in one pass over the keys in tiles, with a running reference m, sum and weighted sum per row, all in 32 bits.
+//
+// The rows of the query heads that share a key head are taken together (new tokens x group rows a key head), so that a tile of keys is read once
+// for all of them.  S^T = K Q^T by matrix instructions: a lane then holds keys of ONE row, the row's maximum and sum need an exchange with the
+// lanes of the same column only, and, with a tile's keys put into the instruction's rows in a fitting order, the sixteen-bit weights stand where the
+// second product O^T = V^T P^T takes its right operand: no weight moves between lanes.  V^T is read from LDS by the transposing read (4 keys x 16
+// elements for 16 lanes).  The weights are rounded to the queries' type for that product
+// (the output is rounded to it too; their sum is taken before that, in 32 bits).
+//
+// The reference m is not the maximum itself: it is raised only when a row's maximum passes it by 2^8 in the weights, since raising it costs a
+// multiplication of the whole weighted sum; weights up to 2^8 (in fp16 2^15, with 2^7 for the reference itself, so that small weights stay above
+// what fp16 can hold) round as well as those up to 1.
+//
+// Keys that a row does not see get weight 0 by selection, whatever their score is.  A weight of 0 does not keep a value that is infinite or not a
+// number out of the matrix product, so in tiles in which a row does not see every key such values are taken out on the way to LDS and given to the
+// rows that see them one by one.
+#ifndef DYN_ATTN_H_
+#define DYN_ATTN_H_
+
+#include "dyn_serve.h"
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+using x8 = T __attribute__((ext_vector_type(8)));
+template <typename T>
+using x4 = T __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Kind;
+template <> struct Kind<__bf16> {
+  static constexpr float bias = 0.0f;                     // log2 of the reference's own weight
+  static constexpr uint32_t carry = 0x00800080u;          // added to the bits without sign, bit 15 tells an exponent of all ones
+  static constexpr uint32_t fraction = 0x007f007fu;
+};
+template <> struct Kind<_Float16> {
+  static constexpr float bias = 7.0f;
+  static constexpr uint32_t carry = 0x04000400u;
+  static constexpr uint32_t fraction = 0x03ff03ffu;
+};
+constexpr float kRaise = 8.0f;
+
+// 16 bytes of a row, as they lie in the cache: 8 elements of 16 bits, or 16 of 8.  What LDS holds is 16 bits either way (every e4m3 value is one of
+// both types).
+__device__ __forceinline__ u32x4 widen(__bf16, uint32_t lo, uint32_t hi) {
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  const v2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const v2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
+}
+__device__ __forceinline__ u32x4 widen(_Float16, uint32_t lo, uint32_t hi) {
+  typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+  const v2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const v2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
+}
+
+// What the waves of a block share of a request: the keys its row tile sees, as tiles of KT keys without those between the first tokens and the window.
+struct Keys {
+  int32_t sink_tiles, first;  // tile v is v below sink_tiles, else v - sink_tiles + first
+  int32_t count;
+};
+template <int KT>
+__device__ __forceinline__ Keys keys_of(const AttnArgs& a, int32_t lo, int32_t hi) {   // positions of the first and last row, hi >= 0
+  Keys k = {0, 0, hi / KT + 1};
+  if (a.window > 0) {
+    const int32_t first = max(0, lo - a.window + 1) / KT, sinks = (int32_t)(((int64_t)a.n_sink + KT - 1) / KT);
+    if (first > sinks) {
+      k.sink_tiles = sinks;
+      k.first = first;
+      k.count = sinks + hi / KT - first + 1;
+    }
+  }
+  return k;
+}
+// The pieces that the tiles are cut into: the last one has what is left.
+__device__ __forceinline__ int pieces_of(const Keys& k, int32_t n_chunk, int32_t each) { return max(1, min(n_chunk, (k.count + each - 1) / each)); }
+__device__ __forceinline__ int32_t tile_of(const Keys& k, int32_t v) { return v < k.sink_tiles ? v : v - k.sink_tiles + k.first; }
+
+// Whether some row from position `first` to `last` does not see every key of a tile.
+template <int KT>
+__device__ __forceinline__ bool hides(const AttnArgs& a, int32_t first, int32_t last, int32_t key0) {
+  return key0 + KT - 1 > first || (a.window > 0 && key0 <= last - a.window && key0 + KT > a.n_sink);
+}
+
+// A request as a block sees it; lengths and offsets are cut to what the arrays hold.
+struct Request { int32_t t0, n, len; };
+__device__ __forceinline__ Request request_of(const AttnArgs& a, int b) {
+  Request q;
+  q.t0 = min(max(a.cu[b], 0), a.n_token);
+  q.n = max(min(a.cu[b + 1], a.n_token) - q.t0, 0);
+  q.len = (int32_t)min((int64_t)max(a.kv_len[b], 0), (int64_t)a.max_pages << a.page_shift);
+  return q;
+}
+
+// The last request for which `holds`, which holds for the first one and for none after one that it does not hold for; 64 places at a time, all lanes of
+// the wave together.
+template <typename P>
+__device__ __forceinline__ int last_request(int n_req, P holds) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_req - 1;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64;
+    const int k = __popcll(__ballot(holds(min(lo + (lane + 1) * step, hi))));      // the first k places
+    const int to = k == 64 ? hi : min(lo + (k + 1) * step, hi) - 1;
+    lo = min(lo + k * step, hi);
+    hi = max(to, lo);
+  }
+  return lo;
+}
+
+// The scores' factor (log2(e) x scale x the key head's), above 0, so that -inf times it is -inf.  The running reference is a maximum: where the factor is
+// negative its sign goes into the queries, exactly.
+__device__ __forceinline__ float factor_of(const AttnArgs& a, int kvh) {
+  return a.scale * (a.k_scale ? a.k_scale[kvh] : 1.0f) * 1.4426950408889634f;
+}
+__device__ __forceinline__ float size_of(float factor) { return fmaxf(fabsf(factor), 1e-30f); }
+
+// 8 elements of a query row.
+template <typename T>
+__device__ __forceinline__ x8<T> load_query(const AttnArgs& a, const T* src, bool in, uint32_t flip) {
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (in) {
+    if (a.q_vec) {
+      v = *(const u32x4*)src;
+    } else {
+      const uint16_t* p = (const uint16_t*)src;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = p[2 * j] | (uint32_t)p[2 * j + 1] << 16;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] ^= flip;
+  }
+  return __builtin_bit_cast(x8<T>, v);
+}
+
+// 4 neighbouring elements of an output row.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* x, bool vec) {
+  if (vec) {
+    x4<T> v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (T)x[i];
+    *(x4<T>*)p = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = (T)x[i];
+  }
+}
+
+// Where a row's pieces lie: token and head.
+__device__ __forceinline__ int64_t part_row(const AttnArgs& a, int chunk, int64_t t, int head) {
+  return ((int64_t)chunk * a.n_token + t) * (a.n_kv_head * a.group) + head;
+}
+
+// The page of a key; an entry outside the cache is read as page 0 and reported.
+__device__ __forceinline__ int32_t checked(const AttnArgs& a, int32_t entry) {
+  if ((uint32_t)entry >= (uint32_t)a.n_page) {
+    atomicOr(&a.header->status, DYN_WS_BAD_PAGE);
+    return 0;
+  }
+  return entry;
+}
+__device__ __forceinline__ int32_t page_of(const AttnArgs& a, int b, int32_t key) {
+  return checked(a, a.table[(size_t)b * a.max_pages + (key >> a.page_shift)]);
+}
+// The same for a key that is the same in all lanes: a scalar load, which waits for none of the vector loads in flight.
+__device__ __forceinline__ int32_t page_of_all(const AttnArgs& a, int b, int32_t key) {
+  typedef const __attribute__((address_space(4))) int32_t* constant;
+  return checked(a, ((constant)a.table)[(size_t)b * a.max_pages + (key >> a.page_shift)]);
+}
+// Tiles whose keys are all there, in pages of 16 tokens and more, are read with one address for 16 keys and a lane's own offset from it.
+__device__ __forceinline__ bool by_sixteen(const AttnArgs& a, int32_t key0, int keys, int32_t len) { return a.page_shift >= 4 && key0 + keys <= len; }
+
+// Where a key's row begins in the cache, in bytes; `page`: the key's.
+__device__ __forceinline__ int64_t row_at(const AttnArgs& a, int kvh, int32_t key, int32_t page, int row_bytes) {
+  return ((((int64_t)page * a.n_kv_head + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * row_bytes;
+}
+
+// 8 values on their way to LDS.  Those that are not finite are taken out and marked, a bit for +inf (`up`) and one for -inf (`down`), both for what is not a
+// number.
+template <typename T>
+__device__ __forceinline__ u32x4 take_out(u32x4 x, uint8_t* up_to, uint8_t* down_to) {
+  uint32_t up = 0, down = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t bits = x[i], odd = (((bits & 0x7fff7fffu) + Kind<T>::carry) & 0x80008000u) >> 15;           // 1 in the halves that are not finite
+    const uint32_t nan = (((bits & Kind<T>::fraction) + 0x7fff7fffu) & 0x80008000u) >> 15, neg = (bits >> 15) & 0x00010001u;
+    const uint32_t u = odd & (nan | (neg ^ 0x00010001u)), d = odd & (nan | neg);
+    up |= ((u | u >> 15) & 3u) << 2 * i;
+    down |= ((d | d >> 15) & 3u) << 2 * i;
+    x[i] = bits & ~(odd * 0xffffu);
+  }
+  *up_to = (uint8_t)up;
+  *down_to = (uint8_t)down;
+  return x;
+}
+// What two marks are worth; both: not a number.
+__device__ __forceinline__ float marked_value(uint32_t up, uint32_t down, int bit) {
+  return (up >> bit & 1u ? INFINITY : 0.0f) - (down >> bit & 1u ? INFINITY : 0.0f);
+}
+
+// The left operand of the second product: 8 keys of one element, by two transposing reads of 4 keys each; lane i of 16 gives the address of key i / 4's elements
+// 4 (i % 4) .. and gets the 4 keys of element i.
+__device__ __forceinline__ u32x4 read_values(const u32x4* lo, const u32x4* hi, int half) {
+  typedef __attribute__((address_space(3))) s16x4* lds4;
+  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((const s16x4*)lo + half));
+  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((const s16x4*)hi + half));
+  return __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+}  // namespace
+
+hipError_t dyn_launch_attend_narrow(const AttnArgs& a, hipStream_t s);
+hipError_t dyn_launch_attend_wide(const AttnArgs& a, hipStream_t s);
+
+#endif  // DYN_ATTN_H_

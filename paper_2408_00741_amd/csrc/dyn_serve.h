@@ -37,16 +37,14 @@ struct AttnArgs {
   float scale;
   int32_t type, cache_type;
   bool q_vec, o_vec;              // 16-byte loads of queries, 8-byte stores of outputs are aligned
-  int32_t max_new;
+  int32_t rows_narrow;            // requests of at most as many rows (new tokens x query heads of a key head) take the narrow kernel, 16 or 32
   // the key axis is cut in at most n_chunk pieces of `tiles` tiles (narrow: requests of few rows, wide: the others)
   int32_t n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide;
   int32_t n_tile_wide;            // row tiles of the wide kernel at most, 0: none
   float* part; float* part_ml;    // workspace: [chunk][token][head][head_dim] and [chunk][token][head][2]
-  uint32_t* arrived_narrow; uint32_t* arrived_wide;   // zero between calls
   WsHeader* header;
 };
 hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s);
-#define DYN_ATTN_ROWS 32          // rows (new tokens x query heads of a key head) of one wave; requests of at most as many take the narrow kernel
 #define DYN_ATTN_KEYS_NARROW 32   // keys of a tile
 #define DYN_ATTN_KEYS_WIDE 64
 #define DYN_ATTN_WAVES_WIDE 4     // waves of a block of the wide kernel, each with rows of its own

@@ -127,10 +127,9 @@ namespace {
 
 // The pieces that the key axis is cut into, for the narrow and the wide kernel, and the places in the workspace.
 struct AttnShape {
-  int32_t n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
+  int32_t rows_narrow, n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
   size_t ml, part, total;
 };
-constexpr int64_t kCounters = 16384;         // words of arrivals; launches that would need more are not cut
 constexpr size_t kPartBytes = 64u << 20;     // pieces' sums at most
 
 AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t max_new, int32_t max_kv, int32_t window,
@@ -151,16 +150,19 @@ AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int3
     chunks = std::max(chunks, c);   // the workspace holds as many as were wanted: never fewer for more keys
   };
   const int64_t narrow = (int64_t)n_req * n_kv_head;
-  cut(narrow, narrow <= kCounters / 2 ? 1024 : 1, (seen + DYN_ATTN_KEYS_NARROW - 1) / DYN_ATTN_KEYS_NARROW, 4, 4, &s.n_chunk_narrow, &s.tiles_narrow);
+  cut(narrow, 1024, (seen + DYN_ATTN_KEYS_NARROW - 1) / DYN_ATTN_KEYS_NARROW, 4, 4, &s.n_chunk_narrow, &s.tiles_narrow);
   s.n_tile_wide = 0;
   s.n_chunk_wide = s.tiles_wide = 1;
-  if (rows > DYN_ATTN_ROWS) {
+  // Steps of up to 32 rows a request take the narrow kernel alone, with 16 rows in half the registers where that is enough; where some request has more, those
+  // of 17 to 32 go with them.
+  s.rows_narrow = rows > 16 && rows <= 32 ? 32 : 16;
+  if (rows > 32) {
     const int64_t R = 32 * DYN_ATTN_WAVES_WIDE, all = (int64_t)n_token * group;
     s.n_tile_wide = (int32_t)(all / R + n_req);
     const int64_t blocks = std::max<int64_t>(1, all / R) * n_kv_head;
-    cut(blocks, (int64_t)s.n_tile_wide * n_kv_head <= kCounters / 2 ? 512 : 1, (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE, 4, 1, &s.n_chunk_wide, &s.tiles_wide);
+    cut(blocks, 512, (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE, 4, 1, &s.n_chunk_wide, &s.tiles_wide);
   }
-  s.ml = 256 + kCounters * sizeof(uint32_t);
+  s.ml = 256;
   s.part = s.ml + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * 2 * sizeof(float)) : 0);
   s.total = s.part + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * head_dim * sizeof(float)) : 0);
   return s;
@@ -200,11 +202,10 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.n_req = p->n_req; a.n_token = p->n_token; a.n_kv_head = p->n_kv_head; a.group = (int32_t)group; a.head_dim = p->head_dim;
   a.page_shift = shift; a.n_page = p->n_page; a.max_pages = p->max_pages; a.window = p->window; a.n_sink = p->n_sink;
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
-  a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.max_new = p->max_new;
+  a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow;
   a.n_chunk_narrow = s.n_chunk_narrow; a.tiles_narrow = s.tiles_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;
   char* base = (char*)workspace;
   a.header = (WsHeader*)base;
-  a.arrived_narrow = (uint32_t*)(base + 256); a.arrived_wide = a.arrived_narrow + kCounters / 2;
   a.part_ml = (float*)(base + s.ml); a.part = (float*)(base + s.part);
   return hip_ok(dyn_launch_paged_attention(a, (hipStream_t)hip_stream), "attention launch") ? DYN_OK : DYN_E_DEVICE;
 }

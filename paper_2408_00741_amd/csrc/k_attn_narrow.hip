@@ -1,0 +1,347 @@
+// Attention for requests of few rows (new tokens x query heads of a key head): one new token each, or a few.
+#include "dyn_attn.h"
+
+namespace {
+
+__device__ __forceinline__ f32x4 mfma(x8<__bf16> a, x8<__bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma(x8<_Float16> a, x8<_Float16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+constexpr int KT = DYN_ATTN_KEYS_NARROW;   // 32 keys: two of the first product's left operands, one of the second product's steps
+
+// Row n (lane % 16) of left operand t is key 8 (n / 4) + 4 t + n % 4 of the tile: lane group g = lane / 16 then has the scores of keys 8 g + 4 t + i, the 8
+// neighbouring keys that the second product wants of it.
+__device__ __forceinline__ int key_of_row(int t, int n) { return 8 * (n >> 2) + 4 * t + (n & 3); }
+
+// Where 8 elements of a value row lie in LDS, in units of 16 bytes: turned by the key so that the 4 keys x 32 bytes that two lane groups (keys 8 apart) read at
+// a time hit all 64 banks.
+template <int DP>
+constexpr int kRow = DP / 8;
+template <int DP>
+__device__ __forceinline__ int v_at(int key, int c8) {
+  return DP == 128 ? key * 16 + (c8 ^ ((key & 3) << 2) ^ ((key >> 3 & 1) << 1)) : key * 8 + (c8 ^ ((key >> 1 & 1) << 2) ^ ((key >> 3 & 1) << 1));
+}
+
+template <typename T, int DP, int NT>
+struct Rows {
+  x8<T> q[NT][DP / 32];      // right operand of the first product: row lane % 16
+  f32x4 o[NT][DP / 16];      // O^T: element 16 t + 4 (lane / 16) + i
+  float m[NT], sum[NT], c;   // reference (before c), sum of this lane's weights, the scores' factor
+  int32_t pos[NT], low[NT];  // position (-1: no row), last key that the window hides
+  int32_t first, last;       // least and greatest position
+};
+
+// Two left operands straight from the cache, 16 bytes a load.  In 8 bits a load is two steps of the product: step d takes the elements
+// 64 (d / 2) + 16 g + 8 (d % 2) .. of a head, in the queries too.
+template <typename T, bool F8, int DP>
+struct KeyRows {
+  static constexpr int kLoads = F8 ? DP / 64 : DP / 32;
+  u32x4 x[2][kLoads];
+  static __device__ __forceinline__ int element(int d, int g) { return F8 ? 64 * (d / 2) + 16 * g + 8 * (d % 2) : 32 * d + 8 * g; }
+  __device__ __forceinline__ void load(const char* const* at, int row_bytes) {   // at[t]: this lane's row of operand t
+    const int c = 16 * ((threadIdx.x >> 4) & 3);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) x[t][i] = *(const u32x4*)(at[t] + (64 * i + c < row_bytes ? 64 * i + c : 0));
+  }
+  template <int NT>
+  __device__ __forceinline__ void scores(int row_bytes, const Rows<T, DP, NT>& r, f32x4 (*s)[2]) {
+    if (row_bytes < 64 * kLoads) {          // beyond the head's end: zeros, as in the queries
+      const int c = 16 * ((threadIdx.x >> 4) & 3);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) x[t][i] = 64 * i + c < row_bytes ? x[t][i] : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        u32x4 k;
+        if constexpr (F8) k = d % 2 ? widen(T{}, x[t][d / 2][2], x[t][d / 2][3]) : widen(T{}, x[t][d / 2][0], x[t][d / 2][1]);
+        else k = x[t][d];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][t] = mfma(__builtin_bit_cast(x8<T>, k), r.q[n][d], s[n][t]);
+      }
+    }
+  }
+};
+
+// A tile of values on its way to LDS, 16 bytes a load, whole rows by neighbouring lanes.
+template <typename T, bool F8, int DP>
+struct Values {
+  static constexpr int kPerRow = F8 ? DP / 16 : DP / 8, kRows = 64 / kPerRow, kEach = KT / kRows;
+  u32x4 x[kEach];
+  __device__ __forceinline__ void write(u32x4* lds, bool mark, uint8_t* marks) {
+    const int lane = threadIdx.x & 63, c = lane % kPerRow;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int row = lane / kPerRow + i * kRows;
+#pragma unroll
+      for (int e = 0; e < (F8 ? 2 : 1); ++e) {
+        const int c8 = F8 ? 2 * c + e : c;
+        u32x4 v = F8 ? widen(T{}, x[i][2 * e], x[i][2 * e + 1]) : x[i];
+        if (mark) v = take_out<T>(v, marks + row * (DP / 8) + c8, marks + (KT + row) * (DP / 8) + c8);
+        lds[v_at<DP>(row, c8)] = v;
+      }
+    }
+  }
+};
+
+// From the scores of a tile to the weighted sum of its values in LDS.
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32x4 (*s)[2], const u32x4* lds, bool marked, const uint32_t* marks, int32_t key0) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
+  if (marked) {      // some row does not see every key: what it does not see scores -inf, weight 0 below, whatever the reference
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int32_t from = r.low[n] - key0 - 8 * g, sinks = a.n_sink - key0 - 8 * g, upto = r.pos[n] - key0 - 8 * g;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][t][i] = 4 * t + i > upto || (a.window > 0 && 4 * t + i <= from && 4 * t + i >= sinks) ? -INFINITY : s[n][t][i];
+    }
+  }
+  x8<T> p[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float top = s[n][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[n][i / 4][i % 4]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool raise = (top - r.m[n]) * r.c > kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+    if (__any(raise)) {
+      const float m = fmaxf(r.m[n], top);
+      const float f = r.m[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((r.m[n] - m) * r.c);
+      r.m[n] = m;
+      r.sum[n] *= f;
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.o[n][t][i] *= f;
+    }
+    const float base = Kind<T>::bias - (r.m[n] == -INFINITY ? 0.0f : r.m[n] * r.c);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i / 4][i % 4], r.c, base));
+      sum += w;
+      p[n][i] = (T)w;
+    }
+    r.sum[n] += sum;
+  }
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const int key = 8 * g + (i16 >> 2), c8 = 2 * t + ((i16 & 3) >> 1);
+    const u32x4 v = read_values(&lds[v_at<DP>(key, c8)], &lds[v_at<DP>(key + 4, c8)], i16 & 1);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) r.o[n][t] = mfma(__builtin_bit_cast(x8<T>, v), p[n], r.o[n][t]);
+  }
+  // values that are not finite were taken out and marked: they go to the rows that see their keys
+  if (marked) {
+    uint32_t any = 0;
+    for (int i = lane; i < 2 * KT * DP / 32; i += 64) any |= marks[i];
+    if (__any(any != 0)) {
+      for (int key = 0; key < KT; ++key) {
+        const int32_t at = key0 + key;
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+          const int word = t / 2, shift = 16 * (t % 2) + 4 * g;
+          const uint32_t up = marks[key * (DP / 32) + word] >> shift, down = marks[(KT + key) * (DP / 32) + word] >> shift;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = marked_value(up, down, i);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) r.o[n][t][i] += at <= r.pos[n] && (at > r.low[n] || at < a.n_sink) ? x : 0.0f;
+          }
+        }
+      }
+    }
+  }
+}
+
+// Requests of at most 16 NT rows.  Four waves take the tiles of a piece of the keys in turn, each for all rows, and join at the end.  K goes straight into
+// registers as the left operand, V through LDS; the next tile's loads are in flight while one is worked on.  Bound by the bytes of K and V.
+template <typename T, bool F8, int DP, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attend_narrow_kernel(AttnArgs a) {
+  __shared__ u32x4 s_tile[4][KT * kRow<DP>];           // a wave's values, and at the end the sums of 16 rows
+  __shared__ uint32_t s_marks[4][2 * KT * DP / 32];
+  __shared__ float s_m[4][16 * NT], s_sum[4][16 * NT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % a.n_kv_head, b = blockIdx.x / a.n_kv_head, chunk = blockIdx.y;
+  if (blockIdx.x == 0 && chunk == 0 && tid == 0) a.header->kind = DYN_WS_KIND_WORD;
+  const Request q = request_of(a, b);
+  const int64_t all_rows = (int64_t)q.n * a.group;
+  if (q.n == 0 || all_rows > a.rows_narrow) return;
+  const int32_t rows = (int32_t)all_rows;
+  const Keys keys = q.len > 0 ? keys_of<KT>(a, q.len - q.n, q.len - 1) : Keys{0, 0, 0};
+  const int pieces = pieces_of(keys, a.n_chunk_narrow, a.tiles_narrow);
+  if (chunk >= pieces) return;
+  const int32_t v0 = chunk * a.tiles_narrow, v1 = chunk == a.n_chunk_narrow - 1 ? keys.count : min(keys.count, v0 + a.tiles_narrow);
+  const int row_bytes = a.head_dim * (F8 ? 1 : 2);
+  const float factor = factor_of(a, kvh);
+  Rows<T, DP, NT> r;
+  r.c = size_of(factor);
+  r.first = q.len - q.n;
+  r.last = q.len - 1;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int32_t row = 16 * n + n16, i = min(row, rows - 1) / a.group, h = min(row, rows - 1) - i * a.group;
+    const T* src = (const T*)a.q + (int64_t)(q.t0 + i) * a.q_token + (int64_t)(kvh * a.group + h) * a.q_head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      const int at = KeyRows<T, F8, DP>::element(d, g);
+      r.q[n][d] = load_query<T>(a, src + at, row < rows && at < a.head_dim, factor < 0.0f ? 0x80008000u : 0u);
+    }
+    r.pos[n] = row < rows ? q.len - q.n + i : -1;
+    r.low[n] = a.window > 0 ? r.pos[n] - a.window : -1;
+    r.m[n] = -INFINITY;
+    r.sum[n] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) r.o[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  using V = Values<T, F8, DP>;
+  KeyRows<T, F8, DP> kr;
+  V values;
+  // pages of a tile's first and 17th key (the tile's end may lie beyond the request's)
+  auto pages_at = [&](int32_t v, int32_t* page) {
+    const int32_t key0 = tile_of(keys, v) * KT;
+    page[0] = page_of_all(a, b, key0);
+    page[1] = page_of_all(a, b, min(key0 + 16, q.len - 1));
+  };
+  // this lane's rows of K, and the values' rows, of tile v
+  auto load_keys = [&](int32_t v, const int32_t* page) {
+    const int32_t key0 = tile_of(keys, v) * KT;
+    const char* at[2];
+    if (by_sixteen(a, key0, KT, q.len)) {
+      const char* lo = (const char*)a.k_cache + row_at(a, kvh, key0, page[0], row_bytes);
+      const char* hi = (const char*)a.k_cache + row_at(a, kvh, key0 + 16, page[1], row_bytes);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) at[t] = (n16 < 8 ? lo : hi) + (key_of_row(t, n16) & 15) * row_bytes;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int32_t key = min(key0 + key_of_row(t, n16), q.len - 1);
+        at[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes);
+      }
+    }
+    kr.load(at, row_bytes);
+  };
+  auto load_values = [&](int32_t v, const int32_t* page) {
+    const int32_t key0 = tile_of(keys, v) * KT;
+    const int c = lane % V::kPerRow * 16, off = c < row_bytes ? c : 0;
+    if (by_sixteen(a, key0, KT, q.len)) {
+      const char* lo = (const char*)a.v_cache + row_at(a, kvh, key0, page[0], row_bytes);
+      const char* hi = (const char*)a.v_cache + row_at(a, kvh, key0 + 16, page[1], row_bytes);
+      const uint32_t mine = lane / V::kPerRow * row_bytes + off;
+#pragma unroll
+      for (int i = 0; i < V::kEach; ++i) {
+        const int row = i * V::kRows;
+        values.x[i] = *(const u32x4*)((row < 16 ? lo : hi) + (row & 15) * row_bytes + mine);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V::kEach; ++i) {
+        const int32_t key = min(key0 + lane / V::kPerRow + i * V::kRows, q.len - 1);
+        values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes) + off);
+      }
+    }
+  };
+  u32x4* lds = s_tile[wave];
+  int32_t v = v0 + wave;
+  if (v < v1) {
+    int32_t page[2];
+    pages_at(v, page);
+    load_keys(v, page);
+    load_values(v, page);
+    if (v + 4 < v1) pages_at(v + 4, page);
+    for (; v < v1; v += 4) {
+      const int32_t key0 = tile_of(keys, v) * KT;
+      const bool marked = hides<KT>(a, r.first, r.last, key0);
+      f32x4 s[NT][2];
+      kr.scores(row_bytes, r, s);
+      __builtin_amdgcn_sched_barrier(0);     // what is loaded next takes the registers that are free now, not others
+      if (v + 4 < v1) load_keys(v + 4, page);
+      values.write(lds, marked, (uint8_t*)s_marks[wave]);
+      if (v + 4 < v1) {
+        load_values(v + 4, page);
+        if (v + 8 < v1) pages_at(v + 8, page);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      weigh<T, DP, NT>(a, r, s, lds, marked, s_marks[wave], key0);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // The four waves' sums, O of each in its own tile's place, 16 rows at a time.
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float sum = r.sum[n] + __shfl_xor(r.sum[n], 16);
+    sum += __shfl_xor(sum, 32);
+    if (g == 0) { s_m[wave][16 * n + n16] = r.m[n]; s_sum[wave][16 * n + n16] = sum; }
+  }
+  const int quads = a.head_dim / 4;
+  const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if (16 * n >= rows) break;
+    float* s_o = (float*)s_tile[wave];
+    if (16 * n + n16 < rows) {
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) *(f32x4*)&s_o[n16 * DP + 16 * t + 4 * g] = r.o[n][t];
+    }
+    __syncthreads();
+    for (int u = tid; u < min(rows - 16 * n, 16) * quads; u += 256) {
+      const int in = u / quads, rw = 16 * n + in, d = (u % quads) * 4, i = rw / a.group, head = kvh * a.group + (rw - i * a.group);
+      const int64_t t = q.t0 + i;
+      const float m = fmaxf(fmaxf(s_m[0][rw], s_m[1][rw]), fmaxf(s_m[2][rw], s_m[3][rw]));
+      float total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float mw = s_m[w][rw];
+        if (mw == -INFINITY && s_sum[w][rw] == 0.0f) continue;        // no weight in this wave's tiles
+        const float f = mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mw - m) * r.c);
+        total = __builtin_fmaf(s_sum[w][rw], f, total);
+        const f32x4 o = *(const f32x4*)&((const float*)s_tile[w])[in * DP + d];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(o[j], f, x[j]);
+      }
+      if (pieces == 1) {
+        const bool none = q.len - q.n + i < 0;
+        const float by = vs / total;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = none ? 0.0f : x[j] * by;
+        store4<T>((T*)a.out + t * a.o_token + (int64_t)head * a.o_head + d, x, a.o_vec);
+      } else {
+        const int64_t at = part_row(a, chunk, t, head);
+        *(float4*)(a.part + at * a.head_dim + d) = float4{x[0], x[1], x[2], x[3]};
+        if (d == 0) { a.part_ml[2 * at] = m; a.part_ml[2 * at + 1] = total; }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, bool F8, int DP>
+hipError_t launch_rows(const AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_req * a.n_kv_head, (unsigned)a.n_chunk_narrow);
+  if (a.rows_narrow <= 16) hipLaunchKernelGGL((attend_narrow_kernel<T, F8, DP, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_narrow_kernel<T, F8, DP, 2>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_type(const AttnArgs& a, hipStream_t s) {   // heads are taken as 64 or 128 wide, zeros beyond their end
+  if (a.cache_type == DYN_T_E4M3) return a.head_dim <= 64 ? launch_rows<T, true, 64>(a, s) : launch_rows<T, true, 128>(a, s);
+  return a.head_dim <= 64 ? launch_rows<T, false, 64>(a, s) : launch_rows<T, false, 128>(a, s);
+}
+
+}  // namespace
+
+hipError_t dyn_launch_attend_narrow(const AttnArgs& a, hipStream_t s) { return a.type == DYN_T_BF16 ? launch_type<__bf16>(a, s) : launch_type<_Float16>(a, s); }

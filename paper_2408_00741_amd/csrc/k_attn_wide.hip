@@ -1,0 +1,334 @@
+// Attention for requests of many rows (new tokens x query heads of a key head): chunks of prompts.
+#include "dyn_attn.h"
+
+namespace {
+
+__device__ __forceinline__ f32x16 mfma(x8<__bf16> a, x8<__bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma(x8<_Float16> a, x8<_Float16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+constexpr int KT = DYN_ATTN_KEYS_WIDE;
+
+// Where 8 elements (16 bytes) of a tile lie in LDS, in units of 16 bytes: rows one after the other, the position in the row turned by the row so that the
+// 16 lanes of a read hit all 64 banks: 16 keys' same elements of K, 4 keys' 32 neighbouring elements of V.
+// (Heads of 96 have the rows of 128.)
+template <int DP>
+constexpr int kRow = DP <= 64 ? 8 : 16;
+template <int DP>
+__device__ __forceinline__ int k_at(int key, int c8) {
+  return DP > 64 ? key * 16 + (c8 ^ (key & 15)) : key * 8 + (c8 ^ ((key >> 1) & 7));
+}
+template <int DP>
+__device__ __forceinline__ int v_at(int key, int c8) {
+  return DP > 64 ? key * 16 + (c8 ^ ((key & 3) << 2)) : key * 8 + (c8 ^ (((key >> 1) & 1) << 2));
+}
+
+// One wave's 32 rows and what it has summed up for them.
+template <typename T, int DP>
+struct Rows {
+  x8<T> q[DP / 16];           // right operand of the first product
+  f32x16 o[DP / 32];          // O^T: column lane % 32, element 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4
+  float m, sum, c;            // reference (before c), sum of this lane's weights, log2(e) x scale x key scale
+  int32_t pos, low;           // position (-1: no row), last key that the window hides
+  int32_t first, last;        // least and greatest position in the wave
+};
+
+// Row n (of the first product's left operand) of 32 keys is key swap23(n): bits 2 and 3 swapped.
+__device__ __forceinline__ int swap23(int n) { return (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1); }
+
+// S^T of a tile whose keys are in LDS.
+template <typename T, int DP>
+__device__ __forceinline__ void scores(const Rows<T, DP>& r, const u32x4* lds_k, f32x16* s) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll
+  for (int mt = 0; mt < KT / 32; ++mt) {
+    const int key = 32 * mt + swap23(lane & 31);
+    f32x16 acc = {};
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, lds_k[k_at<DP>(key, 2 * d + h)]), r.q[d], acc);
+    s[mt] = acc;
+  }
+}
+
+// The rest of a tile: from the scores to the weighted sum of the values in LDS (v_at).  `key0`: the first key's position; `marked`: `marks`
+// has two bits of every value (take_out).
+template <typename T, int DP>
+__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16* s, const u32x4* lds_v, bool marked, const uint32_t* marks, int32_t key0) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const bool some_hidden = hides<KT>(a, r.first, r.last, key0);
+  // register i of s[mt] is key 32 mt + 16 (i / 8) + 8 h + i % 8.  What a row does not see scores -inf: weight 0 below, whatever the reference.
+  if (some_hidden) {
+    const int32_t from = r.low - key0 - 8 * h, sinks = a.n_sink - key0 - 8 * h, upto = r.pos - key0 - 8 * h;
+    if (a.window > 0) {
+#pragma unroll
+      for (int mt = 0; mt < KT / 32; ++mt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int32_t at = 32 * mt + 16 * (i / 8) + i % 8;
+          s[mt][i] = at > upto || (at <= from && at >= sinks) ? -INFINITY : s[mt][i];
+        }
+    } else {
+#pragma unroll
+      for (int mt = 0; mt < KT / 32; ++mt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[mt][i] = 32 * mt + 16 * (i / 8) + i % 8 > upto ? -INFINITY : s[mt][i];
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int mt = 0; mt < KT / 32; ++mt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[mt][i]);
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const bool raise = (top - r.m) * r.c > kRaise || (r.m == -INFINITY && top > -INFINITY);
+  if (__any(raise)) {
+    const float m = fmaxf(r.m, top);
+    const float f = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((r.m - m) * r.c);
+    r.m = m;
+    r.sum *= f;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r.o[t][i] *= f;
+  }
+  const float base = Kind<T>::bias - (r.m == -INFINITY ? 0.0f : r.m * r.c);
+  x8<T> p[KT / 16];
+  float sum = 0.0f;
+#pragma unroll
+  for (int mt = 0; mt < KT / 32; ++mt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], r.c, base));
+      sum += w;
+      p[2 * mt + i / 8][i % 8] = (T)w;
+    }
+  r.sum += sum;
+
+  // V^T: lane group lane / 16 has elements 16 (group % 2) + .. of keys 8 (group / 2) + ..
+  const int g16 = lane >> 4, i16 = lane & 15;
+  auto value = [&](int st, int t) {
+    const int key = 16 * st + 8 * (g16 >> 1) + (i16 >> 2), c8 = 4 * t + 2 * (g16 & 1) + ((i16 & 3) >> 1);
+    return read_values(&lds_v[v_at<DP>(key, c8)], &lds_v[v_at<DP>(key + 4, c8)], i16 & 1);
+  };
+#pragma unroll
+  for (int st = 0; st < KT / 16; ++st)
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) r.o[t] = mfma(__builtin_bit_cast(x8<T>, value(st, t)), p[st], r.o[t]);
+  // values that are not finite were taken out and marked: they go to the rows that see their keys.
+  if (marked) {
+    uint32_t any = 0;
+    for (int i = lane; i < 2 * KT * DP / 32; i += 64) any |= marks[i];
+    if (__any(any != 0)) {
+      for (int key = 0; key < KT; ++key) {
+        const int32_t at = key0 + key;
+        const bool sees = at <= r.pos && (at > r.low || at < a.n_sink);
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+          const uint32_t up = marks[key * (DP / 32) + t] >> 4 * h, down = marks[(KT + key) * (DP / 32) + t] >> 4 * h;
+          if (!__any(up | down)) continue;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int bit = 8 * (i / 4) + i % 4;
+            r.o[t][i] += sees ? marked_value(up, down, bit) : 0.0f;
+          }
+        }
+      }
+    }
+  }
+}
+
+// Loads one wave's rows: rows base .. base + 31 of the request's `rows` for key head kvh.
+template <typename T, int DP>
+__device__ __forceinline__ void load_rows(const AttnArgs& a, const Request& q, int kvh, int32_t base, int32_t rows, Rows<T, DP>& r) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int32_t row = base + (lane & 31);
+  const bool in = row < rows;
+  const int32_t i = (in ? row : base) / a.group, g = (in ? row : base) - i * a.group;
+  const float factor = factor_of(a, kvh);
+  r.c = size_of(factor);
+  const T* src = (const T*)a.q + (int64_t)(q.t0 + i) * a.q_token + (int64_t)(kvh * a.group + g) * a.q_head;
+#pragma unroll
+  for (int d = 0; d < DP / 16; ++d) r.q[d] = load_query<T>(a, src + 16 * d + 8 * h, in && 16 * d < a.head_dim, factor < 0.0f ? 0x80008000u : 0u);
+  r.pos = in ? q.len - q.n + i : -1;
+  r.low = a.window > 0 ? r.pos - a.window : -1;
+  r.first = q.len - q.n + base / a.group;
+  r.last = q.len - q.n + (min(base + 31, rows - 1)) / a.group;
+  r.m = -INFINITY;
+  r.sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) r.o[t] = f32x16{};
+}
+
+// The part of a tile of keys or values that a lane carries from the cache to LDS, in pieces of 16 bytes, whole rows by neighbouring lanes: a wave's piece i is
+// rows first_row(wave, i) .. of 64 / kPerRow.
+template <typename T, bool F8, int DP, int LANES>
+struct Stage {
+  static constexpr int kPerRow = F8 ? kRow<DP> / 2 : kRow<DP>, kRows = 64 / kPerRow, kEach = KT * kPerRow / LANES;
+  static_assert(kRows <= 16 && KT * kPerRow % LANES == 0, "pieces");
+  u32x4 x[kEach];
+  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kRows + i * (LANES / kPerRow); }
+  // `page`: of the pieces' rows.  Keys beyond the request's last one are read as the last one (no row sees them), pieces beyond the head's end as its first.
+  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, const int32_t* page) {
+    const int row_bytes = a.head_dim * (F8 ? 1 : 2), lane = threadIdx.x & 63, c = lane % kPerRow * 16, off = c < row_bytes ? c : 0;
+    if (by_sixteen(a, key0, KT, len)) {
+      const uint32_t mine = lane / kPerRow * row_bytes + off;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key0 + first_row(wave, i), page[i], row_bytes) + mine);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int32_t key = min(key0 + first_row(wave, i) + lane / kPerRow, len - 1);
+        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes) + off);
+      }
+    }
+  }
+  __device__ __forceinline__ void write_keys(const AttnArgs& a, u32x4* lds, int wave) {
+    const int lane = threadIdx.x & 63, c = lane % kPerRow;
+    if (a.head_dim < 8 * kRow<DP>) {        // beyond the head's end: zeros, as in the queries
+      const bool in = c * 16 < a.head_dim * (F8 ? 1 : 2);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) x[i] = in ? x[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int row = first_row(wave, i) + lane / kPerRow;
+#pragma unroll
+      for (int e = 0; e < (F8 ? 2 : 1); ++e) lds[k_at<DP>(row, F8 ? 2 * c + e : c)] = F8 ? widen(T{}, x[i][2 * e], x[i][2 * e + 1]) : x[i];
+    }
+  }
+  __device__ __forceinline__ void write_values(u32x4* lds, bool mark, uint8_t* marks, int wave) {
+    const int lane = threadIdx.x & 63, c = lane % kPerRow;
+    if (c >= DP / (F8 ? 16 : 8)) return;    // heads of 96: the rest of the row is not read
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int row = first_row(wave, i) + lane / kPerRow;
+#pragma unroll
+      for (int e = 0; e < (F8 ? 2 : 1); ++e) {
+        const int c8 = F8 ? 2 * c + e : c;
+        u32x4 v = F8 ? widen(T{}, x[i][2 * e], x[i][2 * e + 1]) : x[i];
+        if (mark) v = take_out<T>(v, marks + row * (DP / 8) + c8, marks + (KT + row) * (DP / 8) + c8);
+        lds[v_at<DP>(row, c8)] = v;
+      }
+    }
+  }
+};
+
+// Requests of more rows: a block has 32 rows for each of its waves, all waves read the same tiles of 64 keys from LDS, two tiles in turn, the next
+// one's loads in flight while one is worked on.  Bound by the matrix instructions and the exponentials beside them.
+template <typename T, bool F8, int DP>
+__global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kernel(AttnArgs a) {
+  constexpr int NW = DYN_ATTN_WAVES_WIDE, R = 32 * NW, kTile = KT * kRow<DP>;   // 16-byte pieces of K (or V) of a tile
+  __shared__ u32x4 s_tile[2][2 * kTile];
+  __shared__ uint32_t s_marks[2][2 * KT * DP / 32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.x % a.n_kv_head, chunk = blockIdx.y;
+  if (blockIdx.x == 0 && chunk == 0 && tid == 0) a.header->kind = DYN_WS_KIND_WORD;
+  // row tiles are numbered so that request b's begin at cu[b] x group / R + b: the request of a tile follows from cu alone.  Later tiles have more
+  // keys: they come first.
+  const int32_t tile = a.n_tile_wide - 1 - blockIdx.x / a.n_kv_head;
+  auto begin_of = [&](int b) { return (int64_t)min(max(a.cu[b], 0), a.n_token) * a.group / R + b; };
+  const int b = last_request(a.n_req, [&](int b) { return begin_of(b) <= tile; });
+  const Request q = request_of(a, b);
+  const int64_t all_rows = (int64_t)q.n * a.group, base64 = ((int64_t)tile - begin_of(b)) * R;
+  if (all_rows <= a.rows_narrow || base64 < 0 || base64 >= all_rows) return;
+  const int32_t rows = (int32_t)all_rows, base = (int32_t)base64, n_row = min(R, rows - base);
+  const int32_t first = q.len - q.n + base / a.group, last = q.len - q.n + (base + n_row - 1) / a.group;
+  const Keys keys = last >= 0 ? keys_of<KT>(a, first, last) : Keys{0, 0, 0};
+  const int pieces = pieces_of(keys, a.n_chunk_wide, a.tiles_wide);
+  if (chunk >= pieces) return;
+  const int32_t v0 = chunk * a.tiles_wide, v1 = chunk == a.n_chunk_wide - 1 ? keys.count : min(keys.count, v0 + a.tiles_wide);
+  Rows<T, DP> r;
+  const bool idle = base + 32 * wave >= rows;
+  load_rows<T, DP>(a, q, kvh, idle ? 0 : base + 32 * wave, idle ? 0 : rows, r);
+  if (idle) r.last = -1;
+  using S = Stage<T, F8, DP, 64 * NW>;
+  S sk, sv;
+  if (v0 < v1) {
+    int32_t page[S::kEach];       // of this wave's pieces of the next tile
+    auto pages_at = [&](int32_t v) {
+#pragma unroll
+      for (int i = 0; i < S::kEach; ++i) page[i] = page_of_all(a, b, min(tile_of(keys, v) * KT + S::first_row(wave, i), q.len - 1));
+    };
+    auto load = [&](int32_t v) {
+      sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, page);
+      sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, page);
+    };
+    auto marked = [&](int32_t v) { return hides<KT>(a, first, last, tile_of(keys, v) * KT); };
+    auto write = [&](int32_t v) {
+      u32x4* at = s_tile[(v - v0) & 1];
+      sk.write_keys(a, at, wave);
+      sv.write_values(at + kTile, marked(v), (uint8_t*)s_marks[(v - v0) & 1], wave);
+    };
+    pages_at(v0);
+    load(v0);
+    if (v0 + 1 < v1) pages_at(v0 + 1);
+    write(v0);
+    __syncthreads();
+    for (int32_t v = v0; v < v1; ++v) {
+      const u32x4* at = s_tile[(v - v0) & 1];
+      const int32_t key0 = tile_of(keys, v) * KT;
+      if (v + 1 < v1) {
+        load(v + 1);
+        if (v + 2 < v1) pages_at(v + 2);
+      }
+      // none of this wave's rows sees a key of the tile: beyond the last row's, or before the first row's window and after the first tokens
+      if (key0 <= r.last && !(a.window > 0 && key0 + KT - 1 <= r.first - a.window && key0 >= a.n_sink)) {
+        f32x16 s[KT / 32];
+        scores<T, DP>(r, at, s);
+        weigh<T, DP>(a, r, s, at + kTile, marked(v), s_marks[(v - v0) & 1], key0);
+      }
+      if (v + 1 < v1) write(v + 1);
+      __syncthreads();
+    }
+  }
+  const int32_t row = base + 32 * wave + (lane & 31);
+  const int h = lane >> 5;
+  const float sum = r.sum + __shfl_xor(r.sum, 32);
+  if (row < rows) {
+    const int32_t i = row / a.group;
+    const int head = kvh * a.group + (row - i * a.group);
+    const int64_t t = q.t0 + i;
+    const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f;
+    if (pieces == 1) {
+      const bool none = r.pos < 0;
+      const float by = vs / sum;
+#pragma unroll
+      for (int tt = 0; tt < DP / 32; ++tt)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const int d = 32 * tt + 8 * (j / 4) + 4 * h;
+          if (d >= a.head_dim) continue;
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : r.o[tt][j + e] * by;
+          store4<T>((T*)a.out + t * a.o_token + (int64_t)head * a.o_head + d, x, a.o_vec);
+        }
+    } else {
+      const int64_t at = part_row(a, chunk, t, head);
+#pragma unroll
+      for (int tt = 0; tt < DP / 32; ++tt)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const int d = 32 * tt + 8 * (j / 4) + 4 * h;
+          if (d < a.head_dim) *(float4*)(a.part + at * a.head_dim + d) = float4{r.o[tt][j], r.o[tt][j + 1], r.o[tt][j + 2], r.o[tt][j + 3]};
+        }
+      if (h == 0) { a.part_ml[2 * at] = r.m; a.part_ml[2 * at + 1] = sum; }
+    }
+  }
+}
+
+
+template <typename T, bool F8, int DP>
+hipError_t launch(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attend_wide_kernel<T, F8, DP>), dim3((unsigned)a.n_tile_wide * a.n_kv_head, (unsigned)a.n_chunk_wide), dim3(64 * DYN_ATTN_WAVES_WIDE), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, bool F8>
+hipError_t launch_dim(const AttnArgs& a, hipStream_t s) {   // heads are taken as 64, 96 or 128 wide, zeros beyond their end
+  return a.head_dim <= 64 ? launch<T, F8, 64>(a, s) : a.head_dim <= 96 ? launch<T, F8, 96>(a, s) : launch<T, F8, 128>(a, s);
+}
+template <typename T>
+hipError_t launch_type(const AttnArgs& a, hipStream_t s) { return a.cache_type == DYN_T_E4M3 ? launch_dim<T, true>(a, s) : launch_dim<T, false>(a, s); }
+
+}  // namespace
+
+hipError_t dyn_launch_attend_wide(const AttnArgs& a, hipStream_t s) { return a.type == DYN_T_BF16 ? launch_type<__bf16>(a, s) : launch_type<_Float16>(a, s); }

@@ -146,7 +146,6 @@ def test_attention_long_cut_in_pieces(dtype, cache, new, kv):
     ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
     out = c.run(q, workspace=ws)
     c.check(q, out)
-    assert int(ws[256:256 + 65536].max()) == 0                    # the counts are as they were
     assert _dyn().dyn_workspace_status(ws) == 0
     again = c.run(q, workspace=ws)
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))   # the same bits on every run
