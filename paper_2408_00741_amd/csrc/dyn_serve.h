@@ -38,8 +38,12 @@ struct AttnArgs {
   int32_t type, cache_type;
   bool q_vec, o_vec;              // 16-byte loads of queries, 8-byte stores of outputs are aligned
   int32_t rows_narrow;            // requests of at most as many rows (new tokens x query heads of a key head) take the narrow kernel, 16 or 32
-  // the key axis is cut in at most n_chunk pieces of `tiles` tiles (narrow: requests of few rows, wide: the others)
-  int32_t n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide;
+  int32_t rows_most;              // the most rows that a request of the narrow kernel can have
+  int32_t blocks_narrow;          // blocks of the narrow kernel, equal parts of all keys; 0: one for each request and key head
+  int4* cuts;                     // workspace [blocks_narrow]: the pair that goes on beyond a block's part (request, key head, last block, slot), request -1: none
+  float* piece; float* piece_ml;  // workspace: [blocks_narrow][2][rows_narrow][head_dim] and [..][2]
+  // wide kernel: the key axis is cut in at most n_chunk_wide pieces of `tiles_wide` tiles
+  int32_t n_chunk_wide, tiles_wide;
   int32_t n_tile_wide;            // row tiles of the wide kernel at most, 0: none
   float* part; float* part_ml;    // workspace: [chunk][token][head][head_dim] and [chunk][token][head][2]
   WsHeader* header;

@@ -125,44 +125,43 @@ int dyn_rope_append(const dyn_append* p, void* hip_stream) {
 
 namespace {
 
-// The pieces that the key axis is cut into, for the narrow and the wide kernel, and the places in the workspace.
+// How the launches are shaped, and the places in the workspace.
 struct AttnShape {
-  int32_t rows_narrow, n_chunk_narrow, tiles_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
-  size_t ml, part, total;
+  int32_t rows_narrow, rows_most, blocks_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
+  size_t piece_ml, piece, ml, part, total;
 };
-constexpr size_t kPartBytes = 64u << 20;     // pieces' sums at most
+constexpr int32_t kBlocksNarrow = 512;       // two for each compute unit: what is resident at a time
+constexpr int64_t kPairs = 4096;             // requests x key heads from which a block is a pair: the card's own order evens them out, and every block's sum over all requests would cost more
+constexpr size_t kPartBytes = 64u << 20;     // sums of the wide kernel's pieces at most
 
 AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t max_new, int32_t max_kv, int32_t window,
                           int32_t n_sink) {
   AttnShape s;
   const int64_t group = n_q_head / n_kv_head, rows = (int64_t)std::min(max_new, n_token) * group;
   const int64_t seen = window > 0 ? std::min<int64_t>(max_kv, (int64_t)window + max_new + n_sink + 2 * DYN_ATTN_KEYS_WIDE) : max_kv;
-  const int64_t row_bytes = (int64_t)n_token * n_q_head * (head_dim + 2) * 4;
-  int64_t chunks = 1;
-  auto cut = [&](int64_t blocks, int64_t want, int64_t tiles, int64_t least, int64_t step, int32_t* n, int32_t* each) {   // at most n pieces of `each` tiles
-    int64_t c = blocks >= want ? 1 : (want + blocks - 1) / blocks;
-    c = std::min(c, std::max<int64_t>(1, tiles / least));
-    c = std::min<int64_t>(c, std::max<int64_t>(1, (int64_t)kPartBytes / std::max<int64_t>(row_bytes, 1)));
-    int64_t e = (tiles + c - 1) / c;
-    e = std::max<int64_t>(1, (e + step - 1) / step * step);
-    *n = (int32_t)std::max<int64_t>(1, (tiles + e - 1) / e);
-    *each = (int32_t)e;
-    chunks = std::max(chunks, c);   // the workspace holds as many as were wanted: never fewer for more keys
-  };
-  const int64_t narrow = (int64_t)n_req * n_kv_head;
-  cut(narrow, 1024, (seen + DYN_ATTN_KEYS_NARROW - 1) / DYN_ATTN_KEYS_NARROW, 4, 4, &s.n_chunk_narrow, &s.tiles_narrow);
-  s.n_tile_wide = 0;
-  s.n_chunk_wide = s.tiles_wide = 1;
   // Steps of up to 32 rows a request take the narrow kernel alone, with 16 rows in half the registers where that is enough; where some request has more, those
   // of 17 to 32 go with them.
   s.rows_narrow = rows > 16 && rows <= 32 ? 32 : 16;
+  s.rows_most = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rows, s.rows_narrow));
+  s.blocks_narrow = (int64_t)n_req * n_kv_head < kPairs ? kBlocksNarrow : 0;
+  s.n_tile_wide = 0;
+  s.n_chunk_wide = s.tiles_wide = 1;
+  int64_t chunks = 1;
   if (rows > 32) {
-    const int64_t R = 32 * DYN_ATTN_WAVES_WIDE, all = (int64_t)n_token * group;
+    const int64_t R = 32 * DYN_ATTN_WAVES_WIDE, all = (int64_t)n_token * group, tiles = (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE;
     s.n_tile_wide = (int32_t)(all / R + n_req);
     const int64_t blocks = std::max<int64_t>(1, all / R) * n_kv_head;
-    cut(blocks, 512, (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE, 4, 1, &s.n_chunk_wide, &s.tiles_wide);
+    // few row tiles: the keys are cut until there are two blocks for each compute unit, pieces of at least 4 tiles; the workspace holds as many pieces as were
+    // wanted: never fewer for more keys
+    chunks = std::min<int64_t>((512 + blocks - 1) / blocks, std::max<int64_t>(1, tiles / 4));
+    chunks = std::min<int64_t>(chunks, std::max<int64_t>(1, (int64_t)kPartBytes / std::max<int64_t>((int64_t)n_token * n_q_head * (head_dim + 2) * 4, 1)));
+    s.tiles_wide = (int32_t)std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
+    s.n_chunk_wide = (int32_t)std::max<int64_t>(1, (tiles + s.tiles_wide - 1) / s.tiles_wide);
   }
-  s.ml = 256;
+  const size_t pieces = (size_t)s.blocks_narrow * 2 * s.rows_narrow;
+  s.piece_ml = 256 + align256((size_t)s.blocks_narrow * sizeof(int4));
+  s.piece = s.piece_ml + align256(pieces * 2 * sizeof(float));
+  s.ml = s.piece + align256(pieces * head_dim * sizeof(float));
   s.part = s.ml + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * 2 * sizeof(float)) : 0);
   s.total = s.part + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * head_dim * sizeof(float)) : 0);
   return s;
@@ -202,10 +201,11 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.n_req = p->n_req; a.n_token = p->n_token; a.n_kv_head = p->n_kv_head; a.group = (int32_t)group; a.head_dim = p->head_dim;
   a.page_shift = shift; a.n_page = p->n_page; a.max_pages = p->max_pages; a.window = p->window; a.n_sink = p->n_sink;
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
-  a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow;
-  a.n_chunk_narrow = s.n_chunk_narrow; a.tiles_narrow = s.tiles_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;
+  a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow; a.rows_most = s.rows_most;
+  a.blocks_narrow = s.blocks_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;
   char* base = (char*)workspace;
   a.header = (WsHeader*)base;
+  a.cuts = (int4*)(base + 256); a.piece_ml = (float*)(base + s.piece_ml); a.piece = (float*)(base + s.piece);
   a.part_ml = (float*)(base + s.ml); a.part = (float*)(base + s.part);
   return hip_ok(dyn_launch_paged_attention(a, (hipStream_t)hip_stream), "attention launch") ? DYN_OK : DYN_E_DEVICE;
 }

@@ -1,10 +1,9 @@
-// Attention over the paged cache: the launches, and the kernel that joins the pieces of rows whose keys were cut.
+// Attention over the paged cache: the launches, and the kernel that joins the pieces of the wide kernel's rows.
 #include "dyn_attn.h"
 
 namespace {
 
-// Joins the pieces of the rows whose keys were cut, a wave for each row.  The sum goes in the order of the pieces: the same values on every run.  A kernel of
-// its own: a block that waits for the others' pieces, or the last one to come, needs fences over all L2s, which cost more than the launch.
+// Joins the pieces of the wide kernel's rows, a wave for each row.  The sum goes in the order of the pieces: the same values on every run.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int lane = threadIdx.x & 63, heads = a.n_kv_head * a.group;
@@ -17,15 +16,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   if (t < q.t0 || t >= q.t0 + q.n) return;
   const int64_t rows = (int64_t)q.n * a.group;
   const int32_t pos = q.len - q.n + (t - q.t0);
-  int pieces;
-  if (rows <= a.rows_narrow) {
-    pieces = q.len > 0 ? pieces_of(keys_of<DYN_ATTN_KEYS_NARROW>(a, q.len - q.n, q.len - 1), a.n_chunk_narrow, a.tiles_narrow) : 1;
-  } else {
-    constexpr int R = 32 * DYN_ATTN_WAVES_WIDE;
-    const int64_t base = ((int64_t)(t - q.t0) * a.group + (head - kvh * a.group)) / R * R;
-    const int32_t first = q.len - q.n + (int32_t)(base / a.group), last = q.len - q.n + (int32_t)((min(base + R, rows) - 1) / a.group);
-    pieces = last >= 0 ? pieces_of(keys_of<DYN_ATTN_KEYS_WIDE>(a, first, last), a.n_chunk_wide, a.tiles_wide) : 1;
-  }
+  if (rows <= a.rows_narrow) return;
+  constexpr int R = 32 * DYN_ATTN_WAVES_WIDE;
+  const int64_t base = ((int64_t)(t - q.t0) * a.group + (head - kvh * a.group)) / R * R;
+  const int32_t first = q.len - q.n + (int32_t)(base / a.group), last = q.len - q.n + (int32_t)((min(base + R, rows) - 1) / a.group);
+  const int pieces = last >= 0 ? pieces_of(keys_of<DYN_ATTN_KEYS_WIDE>(a, first, last), a.n_chunk_wide, a.tiles_wide) : 1;
   if (pieces == 1) return;
   const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f, c = size_of(factor_of(a, kvh));
   const int64_t step = (int64_t)a.n_token * heads;
@@ -67,7 +62,7 @@ hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.n_tile_wide > 0 && (e = dyn_launch_attend_wide(a, s)) != hipSuccess) return e;
   if (a.rows_narrow >= a.group && (e = dyn_launch_attend_narrow(a, s)) != hipSuccess) return e;
-  if (a.n_chunk_narrow == 1 && a.n_chunk_wide == 1) return e;
+  if (a.n_chunk_wide == 1) return e;
   const dim3 grid((unsigned)(((int64_t)a.n_token * a.n_kv_head * a.group + 3) / 4));
   if (a.type == DYN_T_BF16) hipLaunchKernelGGL((join_kernel<__bf16>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((join_kernel<_Float16>), grid, dim3(256), 0, s, a);
