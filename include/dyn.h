@@ -520,7 +520,7 @@ typedef struct {          /* DEVICE, caller-owned; none may alias an input      
  * requests: a request whose pages, with those of all requests before it, are more than the free ones
  * is refused (its tokens get position and slot -1, nothing of it is stored or seen, DYN_WS_NO_PAGES);
  * requests that need no new page go on.  Released pages are handed out from the next step on.
- * One launch up to 2048 requests, two beyond.  Lengths that cannot be (ctx_len < 0, new_len < -1, a
+ * One launch up to 4096 requests, two beyond.  Lengths that cannot be (ctx_len < 0, new_len < -1, a
  * sum that differs from n_token) raise DYN_WS_BAD_REQUEST.  Workspace DEVICE, 256-byte aligned,
  * dyn_kv_step_workspace bytes.                                                            */
 size_t dyn_kv_step_workspace(int32_t n_req);
@@ -577,9 +577,9 @@ int dyn_rope_append(const dyn_append* args, void* hip_stream);
  * max_new and max_kv bound every request's new tokens and kv_len (HOST; the launch is shaped by
  * them: a kv_len beyond max_kv is right but slower, a request of more new tokens than max_new may be
  * left out).  Rows of a request whose table names a page outside the cache are not valid and raise DYN_WS_BAD_PAGE.
- * Workspace DEVICE, 256-byte aligned, dyn_paged_attention_workspace bytes; it must be zero before its
- * first use and may be used again for any later call as it is left (not by two calls at a time).  Its status bits
- * add up over the calls.                                                                  */
+ * Workspace DEVICE, 256-byte aligned, dyn_paged_attention_workspace bytes (not by two calls at a
+ * time).  Nothing of it has to be cleared for the results; its status bits add up over the calls: a caller that
+ * reads them clears the first 256 bytes before the first call.                            */
 typedef struct {
   int32_t n_req, n_token, n_q_head, n_kv_head, head_dim;
   int32_t type, cache_type, page_tokens, n_page, max_pages;

@@ -282,8 +282,8 @@ def _dp(t: Optional[torch.Tensor], dtype=None, name="tensor"):
 
 
 def _stream(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    # the current stream's handle without a Stream object around it: a microsecond less of every call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 class Profile:
@@ -784,27 +784,19 @@ def dyn_kv_step(ctx_len: torch.Tensor, new_len: torch.Tensor, n_token: int, bloc
     i32 = torch.int32
     r = _KvRequests(B, n_token, page_tokens, free_pages.numel(), block_table.shape[1], _dp(ctx_len, i32, "ctx_len"), _dp(new_len, i32, "new_len"),
                     _dp(block_table, i32, "block_table"), _dp(free_pages, i32, "free_pages"), _dp(free_state, i32, "free_state"))
-    need = dyn_kv_step_workspace(B)
-    # one allocation for what is returned and the workspace, each part 256-byte aligned
-    sizes = (B + 1, B, B, n_token, n_token, 2)
-    up = [(4 * n + 255) // 256 * 256 for n in sizes]
-    own = need if workspace is None else 0
-    base = torch.empty(own + sum(up), dtype=torch.uint8, device=dev)
-    words, at, out = base.view(i32), own // 4, []
-    for n, u in zip(sizes, up):
-        out.append(words[at:at + n])
-        at += u // 4
+    # one allocation for what is returned and the workspace, which comes first
+    own = 0 if workspace is not None else (dyn_kv_step_workspace(B) + 3) // 4
+    base = torch.empty(own + 3 * B + 3 + 2 * n_token, dtype=i32, device=dev)
+    parts = base.split_with_sizes([own, B + 1, B, B, n_token, n_token, 2])
+    p = base.data_ptr() + 4 * own
+    plan = _KvPlan(p, p + 4 * (B + 1), p + 4 * (2 * B + 1), p + 4 * (3 * B + 1), p + 4 * (3 * B + 1 + n_token), p + 4 * (3 * B + 1 + 2 * n_token))
     if workspace is None:
-        workspace = base[:own]
-    p = base.data_ptr() + own
-    ptr = []
-    for u in up:
-        ptr.append(p)
-        p += u
-    plan = _KvPlan(*ptr)
-    _check(_lib.dyn_kv_step(C.byref(r), C.byref(plan), _dp(workspace), workspace.numel(), _stream(stream)), "dyn_kv_step")
-    return {"cu_new": out[0], "kv_len": out[1], "next_len": out[2], "pos": out[3], "slot": out[4], "block_table": block_table,
-            "free_pages": free_pages, "free_state": out[5], "workspace": workspace}
+        workspace, ws, nbytes = parts[0], base.data_ptr(), 4 * own
+    else:
+        ws, nbytes = _dp(workspace), workspace.numel() * workspace.element_size()
+    _check(_lib.dyn_kv_step(C.byref(r), C.byref(plan), ws, nbytes, _stream(stream)), "dyn_kv_step")
+    return {"cu_new": parts[1], "kv_len": parts[2], "next_len": parts[3], "pos": parts[4], "slot": parts[5], "block_table": block_table,
+            "free_pages": free_pages, "free_state": parts[6], "workspace": workspace}
 
 
 def dyn_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = DYN_ROPE_PLAIN, factor: float = 1.0, original_tokens: float = 0.0,
@@ -849,8 +841,8 @@ def dyn_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of every request's new tokens over its pages; returns [n_token][n_q_head][head_dim].  max_new and max_kv: at least the
     greatest number of new tokens and the greatest kv_len (max_new is n_token, max_kv what the table holds, where the caller does not know better).
-    scale: 1 / sqrt(head_dim) by default.  A caller that keeps a workspace (dyn_paged_attention_workspace bytes, zero when it is made) saves an
-    allocation and a fill per call."""
+    scale: 1 / sqrt(head_dim) by default.  A caller that keeps a workspace (dyn_paged_attention_workspace bytes, its first 256 zero when it is made)
+    saves an allocation and a fill per call, and can read its status."""
     if q.dim() != 3 or block_table.dim() != 2:
         raise ValueError("q must be [n_token][n_q_head][head_dim], block_table [n_req][max_pages]")
     T, H, D = q.shape
@@ -862,10 +854,11 @@ def dyn_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     if out is None:
         out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
     if workspace is None:
-        workspace = torch.zeros(max(256, dyn_paged_attention_workspace(B, T, H, G, D, max_new, max_kv)), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(256, dyn_paged_attention_workspace(B, T, H, G, D, max_new, max_kv)), dtype=torch.uint8, device=q.device)
+        workspace[:256].zero_()
     a = _Attention(B, T, H, G, D, _type(q, "q"), ct, P, N, block_table.shape[1], max_new, max_kv, window, n_sink,
                    D ** -0.5 if scale is None else scale, _rows(q, "q", q.shape, q.dtype), _rows(out, "out", (T, H, D), q.dtype), kc, vc,
                    _scale(k_scale, G, "k_scale"), _scale(v_scale, G, "v_scale"), _dp(block_table, torch.int32, "block_table"),
                    _dp(cu_new, torch.int32, "cu_new"), _dp(kv_len, torch.int32, "kv_len"))
-    _check(_lib.dyn_paged_attention(C.byref(a), _dp(workspace), workspace.numel(), _stream(stream)), "dyn_paged_attention")
+    _check(_lib.dyn_paged_attention(C.byref(a), _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "dyn_paged_attention")
     return out

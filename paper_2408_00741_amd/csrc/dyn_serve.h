@@ -13,7 +13,7 @@ struct KvStepArgs {
   WsHeader* header;
 };
 hipError_t dyn_launch_kv_step(const KvStepArgs& a, hipStream_t s);
-#define DYN_KV_ONE_LAUNCH 2048    // requests whose sums every block makes for itself
+#define DYN_KV_ONE_LAUNCH 4096    // requests whose sums every block makes for itself
 
 #define DYN_ROPE_MAX_PAIRS 64     // head_dim / 2 at most: the frequencies travel in the kernel's arguments
 struct RopeArgs {

@@ -143,7 +143,9 @@ AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int3
   // of 17 to 32 go with them.
   s.rows_narrow = rows > 16 && rows <= 32 ? 32 : 16;
   s.rows_most = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rows, s.rows_narrow));
-  s.blocks_narrow = (int64_t)n_req * n_kv_head < kPairs ? kBlocksNarrow : 0;
+  // a block for each unit (four tiles of keys) where they are few
+  const int64_t pairs = (int64_t)n_req * n_kv_head, units = pairs * ((seen + 4 * DYN_ATTN_KEYS_NARROW - 1) / (4 * DYN_ATTN_KEYS_NARROW) + 1);
+  s.blocks_narrow = pairs < kPairs ? (int32_t)std::min<int64_t>(kBlocksNarrow, units) : 0;
   s.n_tile_wide = 0;
   s.n_chunk_wide = s.tiles_wide = 1;
   int64_t chunks = 1;

@@ -197,7 +197,8 @@ __device__ __forceinline__ Share share_of(const AttnArgs& a) {
   }
   const int lane = threadIdx.x & 63;
   s.all = 0;
-  for (int b0 = 0; b0 < a.n_req; b0 += 64) s.all += units_of(a, b0 + lane);
+  int32_t u = 0;           // of the last 64 requests: all there are in most calls
+  for (int b0 = 0; b0 < a.n_req; b0 += 64) s.all += u = units_of(a, b0 + lane);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) s.all += __shfl_xor(s.all, d);
   s.all = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s.all >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)s.all));   // known to be the same in all lanes
@@ -210,7 +211,7 @@ __device__ __forceinline__ Share share_of(const AttnArgs& a) {
   s.end = s.all * (blockIdx.x + 1) / s.blocks;
   int64_t before = 0;      // units of the requests before
   for (int b0 = 0; b0 < a.n_req; b0 += 64) {
-    const int32_t u = units_of(a, b0 + lane);
+    if (a.n_req > 64) u = units_of(a, b0 + lane);
     int64_t upto = (int64_t)u * a.n_kv_head;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {

@@ -8,52 +8,64 @@ namespace {
 
 // What a request's lengths ask for; lengths that cannot be are cut to what can, and reported.
 struct Ask { int32_t ctx, n, have, need, back; bool bad, too_long; };
+__device__ __forceinline__ uint32_t columns_of(const KvStepArgs& a, uint32_t tokens) { return (tokens + ((1u << a.page_shift) - 1u)) >> a.page_shift; }
 __device__ __forceinline__ Ask ask_of(const KvStepArgs& a, int b) {
   Ask r;
-  int32_t c = a.ctx_len[b], n = a.new_len[b];
-  const int64_t cap = (int64_t)a.max_pages << a.page_shift;
-  const int32_t up = (1 << a.page_shift) - 1;
-  r.bad = c < 0 || c > cap || n < -1;
-  c = (int32_t)min((int64_t)max(c, 0), cap);
-  r.have = (int32_t)(((int64_t)c + up) >> a.page_shift);
+  const int32_t c = a.ctx_len[b], n = a.new_len[b];
+  const uint32_t cap = (uint32_t)a.max_pages << a.page_shift;       // below 2^31, as are both lengths: their sum is below 2^32
+  r.bad = c < 0 || (uint32_t)c > cap || n < -1;
+  r.ctx = (int32_t)min((uint32_t)max(c, 0), cap);
+  r.have = (int32_t)columns_of(a, (uint32_t)r.ctx);
   r.back = n == -1 ? r.have : 0;
-  n = max(n, 0);
-  r.too_long = (int64_t)c + n > cap;
-  r.need = r.too_long ? 0 : (int32_t)(((int64_t)c + n + up) >> a.page_shift) - r.have;
-  r.ctx = c;
-  r.n = n;
+  r.n = max(n, 0);
+  r.too_long = (uint32_t)r.ctx + (uint32_t)r.n > cap;
+  r.need = r.too_long ? 0 : (int32_t)columns_of(a, (uint32_t)r.ctx + (uint32_t)r.n) - r.have;
   return r;
 }
-
 __device__ __forceinline__ int32_t cached_of(const KvStepArgs& a, int b) {   // -1: more tokens than the row has columns
   const Ask q = ask_of(a, b);
   return q.too_long ? -1 : q.ctx;
 }
 
-struct Sums { int64_t n; int32_t need, back; };
-__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {x.n + y.n, x.need + y.need, x.back + y.back}; }
+// New tokens (as an unsigned sum that stays at 2^32 - 1 once it is there: n_token is less), pages asked for, pages given back.
+struct Sums { uint32_t n; int32_t need, back; };
+__device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {add_sat(x.n, y.n), x.need + y.need, x.back + y.back}; }
 
-// Sums over the threads before this one; `total` over all.  s_wave: one Sums per wave.
-template <int THREADS>
-__device__ __forceinline__ Sums before_of(Sums v, Sums* s_wave, Sums* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Sums in = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const Sums o = {__shfl_up(in.n, d), __shfl_up(in.need, d), __shfl_up(in.back, d)};
-    if (lane >= d) in = in + o;
-  }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ Sums moved(const Sums& v) {      // 0 where no lane is that far back
+  return {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)v.n, CTRL, ROWS, 0xF, false), __builtin_amdgcn_update_dpp(0, v.need, CTRL, ROWS, 0xF, false),
+          __builtin_amdgcn_update_dpp(0, v.back, CTRL, ROWS, 0xF, false)};
+}
+
+// Sums over the lanes up to this one; all lanes active.
+__device__ __forceinline__ Sums upto_lane(Sums in) {
+  in = in + moved<0x111, 0xF>(in);   // row_shr:1, 2, 4, 8: inside the rows of 16 lanes
+  in = in + moved<0x112, 0xF>(in);
+  in = in + moved<0x114, 0xF>(in);
+  in = in + moved<0x118, 0xF>(in);
+  in = in + moved<0x142, 0xA>(in);   // row_bcast:15 into rows 1 and 3
+  in = in + moved<0x143, 0xC>(in);   // row_bcast:31 into rows 2 and 3
+  return in;
+}
+__device__ __forceinline__ Sums of_lane(const Sums& v, int lane) {
+  return {(uint32_t)__builtin_amdgcn_readlane((int)v.n, lane), __builtin_amdgcn_readlane(v.need, lane), __builtin_amdgcn_readlane(v.back, lane)};
+}
+// Sums over the waves before this one, and over all.  s_wave: one Sums per wave.
+template <int WAVES>
+__device__ __forceinline__ Sums before_wave(const Sums& mine, Sums* s_wave, Sums* total) {
+  const int wave = threadIdx.x >> 6;
   __syncthreads();
-  if (lane == 63) s_wave[wave] = in;
+  if ((threadIdx.x & 63) == 0) s_wave[wave] = mine;
   __syncthreads();
   Sums base = {0, 0, 0}, all = {0, 0, 0};
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     if (w == wave) base = all;
     all = all + s_wave[w];
   }
   *total = all;
-  return {base.n + in.n - v.n, base.need + in.need - v.need, base.back + in.back - v.back};
+  return base;
 }
 
 // The last b in [lo, hi] with at[b] <= x; at does not decrease, at[lo] <= x.
@@ -61,6 +73,18 @@ __device__ __forceinline__ int last_at(const int32_t* at, int lo, int hi, int32_
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (at[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+// The same for an x that is the same in all lanes of a wave: 64 places at a time.
+__device__ __forceinline__ int last_at_all(const int32_t* at, int lo, int hi, int32_t x) {
+  const int lane = threadIdx.x & 63;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64;
+    const int k = __popcll(__ballot(at[min(lo + (lane + 1) * step, hi)] <= x));
+    const int to = k == 64 ? hi : min(lo + (k + 1) * step, hi) - 1;
+    lo = min(lo + k * step, hi);
+    hi = max(to, lo);
   }
   return lo;
 }
@@ -81,32 +105,40 @@ __device__ __forceinline__ int32_t ring_at(const KvStepArgs& a, const Ring& r, i
 // blocks take in pieces; the request of an item is found by bisection in the sums over the requests before (cu, need, back: [n_req + 1]).
 // Pages handed out and pages given back lie in different parts of the ring, and what a token's slot needs of a new page is read from the
 // ring, not from the table: no block waits for another.
-constexpr int kStepThreads = 256, kStepPiece = 1024;
+constexpr int kStepAhead = 4;     // tokens of a thread at a time: their entries are fetched together
+template <int kStepThreads>
 __device__ __forceinline__ void step_items(const KvStepArgs& a, const Ring& ring, const int32_t* cu, const int32_t* need, const int32_t* back,
                                            const int32_t* s_ctx) {   // s_ctx: cached_of() of every request, or null
   const int tid = threadIdx.x, B = a.n_req, page = 1 << a.page_shift;
   const int32_t n_need = need[B], n_back = back[B], n_tok = cu[B];
-  for (int64_t p0 = (int64_t)blockIdx.x * kStepPiece; p0 < a.n_token; p0 += (int64_t)gridDim.x * kStepPiece) {
-    const int32_t p1 = (int32_t)min(p0 + kStepPiece, (int64_t)a.n_token) - 1;
-    const int lo = last_at(cu, 0, B, (int32_t)p0), hi = last_at(cu, lo, B, p1);
-    for (int32_t t = (int32_t)p0 + tid; t <= p1; t += kStepThreads) {
-      int32_t pos = -1, slot = -1;
-      if (t < n_tok) {
-        const int b = last_at(cu, lo, min(hi, B - 1), t);
+  const int64_t piece = (((int64_t)a.n_token + gridDim.x - 1) / gridDim.x + kStepThreads - 1) / kStepThreads * kStepThreads;
+  const int64_t p0 = blockIdx.x * piece, p1 = min(p0 + piece, (int64_t)a.n_token) - 1;
+  if (p0 <= p1) {
+    const int lo = last_at_all(cu, 0, B, (int32_t)p0), hi = min(last_at_all(cu, lo, B, (int32_t)p1), B - 1);
+    for (int64_t t0 = p0 + tid; t0 <= p1; t0 += kStepAhead * kStepThreads) {
+      int32_t pos[kStepAhead], entry[kStepAhead];
+#pragma unroll
+      for (int i = 0; i < kStepAhead; ++i) {
+        const int64_t t = t0 + i * kStepThreads;
+        pos[i] = -1;
+        entry[i] = -1;
+        if (t > p1 || t >= n_tok) continue;
+        const int b = last_at(cu, min(lo, hi), hi, (int32_t)t);
         const int32_t c = s_ctx ? s_ctx[b] : cached_of(a, b);
-        const int64_t x = (int64_t)c + (t - cu[b]);
-        const int32_t have = (int32_t)(((int64_t)c + page - 1) >> a.page_shift), col = (int32_t)(x >> a.page_shift);
-        const int32_t want = need[b + 1] - need[b];
-        // refused: more tokens than the row has columns, or too few pages
-        const bool ok = c >= 0 && (want == 0 || need[b + 1] <= ring.count) && col < have + want;
-        if (ok) {
-          const int32_t entry = col < have ? a.table[(size_t)b * a.max_pages + col] : a.ring[ring_at(a, ring, need[b] + col - have)];
-          pos = (int32_t)x;
-          if (entry >= 0 && entry < a.n_page) slot = (entry << a.page_shift) + (int32_t)(x & (page - 1));
-        }
+        if (c < 0) continue;                         // refused: more tokens than the row has columns
+        const uint32_t x = (uint32_t)c + (uint32_t)(t - cu[b]);
+        const int32_t have = (int32_t)columns_of(a, (uint32_t)c), col = (int32_t)(x >> a.page_shift), want = need[b + 1] - need[b];
+        if ((want && need[b + 1] > ring.count) || col >= have + want) continue;      // refused: too few pages
+        entry[i] = col < have ? a.table[(size_t)b * a.max_pages + col] : a.ring[ring_at(a, ring, need[b] + col - have)];
+        pos[i] = (int32_t)x;
       }
-      a.pos[t] = pos;
-      a.slot[t] = slot;
+#pragma unroll
+      for (int i = 0; i < kStepAhead; ++i) {
+        const int64_t t = t0 + i * kStepThreads;
+        if (t > p1) continue;
+        a.pos[t] = pos[i];
+        a.slot[t] = entry[i] >= 0 && entry[i] < a.n_page ? (entry[i] << a.page_shift) + (pos[i] & (page - 1)) : -1;
+      }
     }
   }
   const int step = gridDim.x * kStepThreads, at = blockIdx.x * kStepThreads + tid;
@@ -114,7 +146,7 @@ __device__ __forceinline__ void step_items(const KvStepArgs& a, const Ring& ring
     const int b = last_at(need, 0, B - 1, e);
     if (need[b + 1] > ring.count) continue;
     const int32_t c = s_ctx ? s_ctx[b] : cached_of(a, b);
-    const int32_t have = (int32_t)(((int64_t)c + page - 1) >> a.page_shift);
+    const int32_t have = (int32_t)columns_of(a, (uint32_t)c);
     a.table[(size_t)b * a.max_pages + have + (e - need[b])] = a.ring[ring_at(a, ring, e)];
   }
   for (int32_t e = at; e < min(n_back, a.n_page - ring.count); e += step) {
@@ -126,7 +158,7 @@ __device__ __forceinline__ void step_items(const KvStepArgs& a, const Ring& ring
 // What is written once per request, and the free list's new state (by the block that has the sums).
 __device__ __forceinline__ void write_request(const KvStepArgs& a, int b, const Ask& q, const Sums& before, int32_t count) {
   const bool ok = !q.too_long && (q.need == 0 || before.need + q.need <= count), gone = a.new_len[b] == -1;
-  a.cu[b] = (int32_t)min(before.n, (int64_t)a.n_token);
+  a.cu[b] = (int32_t)min(before.n, (uint32_t)a.n_token);
   a.kv_len[b] = ok && !gone ? q.ctx + q.n : 0;
   a.next_len[b] = gone ? 0 : ok ? q.ctx + q.n : q.ctx;
 }
@@ -134,7 +166,7 @@ __device__ __forceinline__ uint32_t status_of(const KvStepArgs& a, const Ask& q,
   return (q.bad ? DYN_WS_BAD_REQUEST : 0u) | (q.too_long || (q.need && before.need + q.need > count) ? DYN_WS_NO_PAGES : 0u);
 }
 __device__ __forceinline__ void write_state(const KvStepArgs& a, const Ring& r, int32_t taken, const Sums& all, uint32_t status) {
-  if (all.n != a.n_token) status |= DYN_WS_BAD_REQUEST;
+  if (all.n != (uint32_t)a.n_token) status |= DYN_WS_BAD_REQUEST;
   if ((int64_t)r.count + all.back > a.n_page) status |= DYN_WS_BAD_PAGE;    // more pages than there are: those beyond are not taken back
   if (a.state[0] != r.first || a.state[1] != r.count) status |= DYN_WS_BAD_PAGE;
   const int64_t f = (int64_t)r.first + taken;
@@ -146,47 +178,54 @@ __device__ __forceinline__ void write_state(const KvStepArgs& a, const Ring& r, 
 }
 
 // Up to DYN_KV_ONE_LAUNCH requests: every block makes all sums for itself, in LDS, and takes its pieces: one launch.  What bounds a step of
-// few tokens is latency: the launch, the lengths, the sums, the table's entry, one after the other.
+// few tokens is latency: the launch, the lengths, the sums, the table's entry, one after the other.  EACH: requests of a thread.
+template <int EACH, int kStepThreads>
 __global__ __launch_bounds__(kStepThreads) void kv_step_kernel(KvStepArgs a) {
-  constexpr int kEach = DYN_KV_ONE_LAUNCH / kStepThreads;
-  __shared__ int32_t s_cu[DYN_KV_ONE_LAUNCH + 1], s_need[DYN_KV_ONE_LAUNCH + 1], s_back[DYN_KV_ONE_LAUNCH + 1], s_ctx[DYN_KV_ONE_LAUNCH];
+  constexpr int kMost = EACH * kStepThreads;
+  __shared__ int32_t s_cu[kMost + 1], s_need[kMost + 1], s_back[kMost + 1], s_ctx[kMost];
   __shared__ Sums s_wave[kStepThreads / 64];
   __shared__ uint32_t s_status;
   __shared__ int32_t s_taken;
-  const int tid = threadIdx.x, B = a.n_req, each = (B + kStepThreads - 1) / kStepThreads;
+  const int tid = threadIdx.x, B = a.n_req;
   if (tid == 0) { s_status = 0u; s_taken = 0; }
   const Ring ring = ring_of(a);
-  Ask q[kEach];
-  Sums mine = {0, 0, 0};
+  // a wave has EACH x 64 requests one after the other
+  const int lane = tid & 63, first = (tid >> 6) * EACH * 64;
+  Ask q[EACH];
+  Sums at[EACH], mine = {0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int b = tid * each + i;
-    if (i < each && b < B) {
-      q[i] = ask_of(a, b);
-      mine = mine + Sums{q[i].n, q[i].need, q[i].back};
-    }
+  for (int i = 0; i < EACH; ++i) {
+    const int b = first + i * 64 + lane;
+    q[i] = ask_of(a, min(b, B - 1));
+    if (b >= B) q[i] = Ask{0, 0, 0, 0, 0, false, false};
   }
-  Sums all, at = before_of<kStepThreads>(mine, s_wave, &all);
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const Sums in = upto_lane(Sums{(uint32_t)q[i].n, q[i].need, q[i].back});
+    at[i] = mine + moved<0x138, 0xF>(in);            // wave_shr:1
+    mine = mine + of_lane(in, 63);
+  }
+  Sums all;
+  const Sums base = before_wave<kStepThreads / 64>(mine, s_wave, &all);
   uint32_t status = 0;
   int32_t taken = 0;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int b = tid * each + i;
-    if (i < each && b < B) {
-      s_cu[b] = (int32_t)min(at.n, (int64_t)a.n_token);
-      s_need[b] = at.need;
-      s_back[b] = at.back;
-      s_ctx[b] = q[i].too_long ? -1 : q[i].ctx;
-      if (blockIdx.x == 0) {
-        write_request(a, b, q[i], at, ring.count);
-        status |= status_of(a, q[i], at, ring.count);
-        if (at.need + q[i].need <= ring.count) taken = at.need + q[i].need;
-      }
-      at = at + Sums{q[i].n, q[i].need, q[i].back};
+  for (int i = 0; i < EACH; ++i) {
+    const int b = first + i * 64 + lane;
+    if (b >= B) continue;
+    const Sums before = base + at[i];
+    s_cu[b] = (int32_t)min(before.n, (uint32_t)a.n_token);
+    s_need[b] = before.need;
+    s_back[b] = before.back;
+    s_ctx[b] = q[i].too_long ? -1 : q[i].ctx;
+    if (blockIdx.x == 0) {
+      write_request(a, b, q[i], before, ring.count);
+      status |= status_of(a, q[i], before, ring.count);
+      if (before.need + q[i].need <= ring.count) taken = before.need + q[i].need;
     }
   }
   if (tid == 0) {
-    s_cu[B] = (int32_t)min(all.n, (int64_t)a.n_token);
+    s_cu[B] = (int32_t)min(all.n, (uint32_t)a.n_token);
     s_need[B] = all.need;
     s_back[B] = all.back;
   }
@@ -199,7 +238,7 @@ __global__ __launch_bounds__(kStepThreads) void kv_step_kernel(KvStepArgs a) {
     a.cu[B] = s_cu[B];
     write_state(a, ring, s_taken, all, s_status);
   }
-  step_items(a, ring, s_cu, s_need, s_back, s_ctx);
+  step_items<kStepThreads>(a, ring, s_cu, s_need, s_back, s_ctx);
 }
 
 // More requests: the sums by one block, through all requests a thousand at a time, then the pieces.
@@ -218,8 +257,9 @@ __global__ __launch_bounds__(kSumThreads) void kv_sums_kernel(KvStepArgs a) {
     const int b = b0 + tid;
     Ask q = {0, 0, 0, 0, 0, false, false};
     if (b < B) q = ask_of(a, b);
+    const Sums in = upto_lane(Sums{(uint32_t)q.n, q.need, q.back});
     Sums all;
-    const Sums at = carry + before_of<kSumThreads>(Sums{q.n, q.need, q.back}, s_wave, &all);
+    const Sums at = carry + before_wave<kSumThreads / 64>(of_lane(in, 63), s_wave, &all) + moved<0x138, 0xF>(in);
     if (b < B) {
       write_request(a, b, q, at, ring.count);
       a.need[b] = at.need;
@@ -233,30 +273,33 @@ __global__ __launch_bounds__(kSumThreads) void kv_sums_kernel(KvStepArgs a) {
   if (taken) atomicMax(&s_taken, taken);
   __syncthreads();
   if (tid == 0) {
-    a.cu[B] = (int32_t)min(carry.n, (int64_t)a.n_token);
+    a.cu[B] = (int32_t)min(carry.n, (uint32_t)a.n_token);
     a.need[B] = carry.need;
     a.back[B] = carry.back;
     write_state(a, ring, s_taken, carry, s_status);
   }
 }
-__global__ __launch_bounds__(kStepThreads) void kv_items_kernel(KvStepArgs a) {
-  step_items(a, ring_of(a), a.cu, a.need, a.back, nullptr);
+__global__ __launch_bounds__(256) void kv_items_kernel(KvStepArgs a) {
+  step_items<256>(a, ring_of(a), a.cu, a.need, a.back, nullptr);
 }
 
 }  // namespace
 
 hipError_t dyn_launch_kv_step(const KvStepArgs& a, hipStream_t s) {
   DynTimed timed(DYN_K_KV_STEP, s);
-  const int64_t pieces = std::max<int64_t>(((int64_t)a.n_token + kStepPiece - 1) / kStepPiece, (a.n_req + 63) / 64);
-  const unsigned grid = (unsigned)std::min<int64_t>(std::max<int64_t>(pieces, 1), 1024);
-  if (a.n_req <= DYN_KV_ONE_LAUNCH) {
-    hipLaunchKernelGGL(kv_step_kernel, dim3(grid), dim3(kStepThreads), 0, s, a);
-    return hipGetLastError();
+  // a token a thread while that is at most two blocks a compute unit; requests may give back many pages each
+  const int64_t pieces = std::max<int64_t>(((int64_t)a.n_token + 255) / 256, (a.n_req + 3) / 4);
+  auto grid = [&](int64_t most) { return dim3((unsigned)std::min(std::max<int64_t>(pieces, 1), most)); };
+  static_assert(DYN_KV_ONE_LAUNCH == 4 * 1024, "requests of a thread");
+  if (a.n_req <= 256) hipLaunchKernelGGL((kv_step_kernel<1, 256>), grid(512), dim3(256), 0, s, a);
+  else if (a.n_req <= 1024) hipLaunchKernelGGL((kv_step_kernel<4, 256>), grid(512), dim3(256), 0, s, a);
+  else if (a.n_req <= DYN_KV_ONE_LAUNCH) hipLaunchKernelGGL((kv_step_kernel<4, 1024>), grid(256), dim3(1024), 0, s, a);
+  else {
+    hipLaunchKernelGGL(kv_sums_kernel, dim3(1), dim3(kSumThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kv_items_kernel, grid(2048), dim3(256), 0, s, a);
   }
-  hipLaunchKernelGGL(kv_sums_kernel, dim3(1), dim3(kSumThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kv_items_kernel, dim3(grid), dim3(kStepThreads), 0, s, a);
   return hipGetLastError();
 }
 
