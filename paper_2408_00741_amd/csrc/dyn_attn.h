@@ -161,21 +161,22 @@ __device__ __forceinline__ int64_t part_row(const AttnArgs& a, int chunk, int64_
   return ((int64_t)chunk * a.n_token + t) * (a.n_kv_head * a.group) + head;
 }
 
-// The page of a key; an entry outside the cache is read as page 0 and reported.
-__device__ __forceinline__ int32_t checked(const AttnArgs& a, int32_t entry) {
-  if ((uint32_t)entry >= (uint32_t)a.n_page) {
-    atomicOr(&a.header->status, DYN_WS_BAD_PAGE);
-    return 0;
-  }
-  return entry;
+// The page of a key; an entry outside the cache is read as one inside and reported (`bad`).
+__device__ __forceinline__ int32_t inside(const AttnArgs& a, int32_t entry, bool* bad) {
+  const uint32_t page = min((uint32_t)entry, (uint32_t)a.n_page - 1u);
+  *bad |= page != (uint32_t)entry;
+  return (int32_t)page;
 }
-__device__ __forceinline__ int32_t page_of(const AttnArgs& a, int b, int32_t key) {
-  return checked(a, a.table[(size_t)b * a.max_pages + (key >> a.page_shift)]);
+__device__ __forceinline__ int32_t page_of(const AttnArgs& a, int b, int32_t key, bool* bad) {
+  return inside(a, a.table[(size_t)b * a.max_pages + (key >> a.page_shift)], bad);
 }
 // The same for a key that is the same in all lanes: a scalar load, which waits for none of the vector loads in flight.
-__device__ __forceinline__ int32_t page_of_all(const AttnArgs& a, int b, int32_t key) {
+__device__ __forceinline__ int32_t page_of_all(const AttnArgs& a, int b, int32_t key, bool* bad) {
   typedef const __attribute__((address_space(4))) int32_t* constant;
-  return checked(a, ((constant)a.table)[(size_t)b * a.max_pages + (key >> a.page_shift)]);
+  return inside(a, ((constant)a.table)[(size_t)b * a.max_pages + (key >> a.page_shift)], bad);
+}
+__device__ __forceinline__ void report(const AttnArgs& a, bool bad) {
+  if (bad) atomicOr(&a.header->status, DYN_WS_BAD_PAGE);
 }
 // Tiles whose keys are all there, in pages of 16 tokens and more, are read with one address for 16 keys and a lane's own offset from it.
 __device__ __forceinline__ bool by_sixteen(const AttnArgs& a, int32_t key0, int keys, int32_t len) { return a.page_shift >= 4 && key0 + keys <= len; }
@@ -203,6 +204,12 @@ __device__ __forceinline__ u32x4 take_out(u32x4 x, uint8_t* up_to, uint8_t* down
   *down_to = (uint8_t)down;
   return x;
 }
+// A value the compiler takes as a new one: what is computed from it is computed where it stands, not held in registers from before a loop.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // What two marks are worth; both: not a number.
 __device__ __forceinline__ float marked_value(uint32_t up, uint32_t down, int bit) {
   return (up >> bit & 1u ? INFINITY : 0.0f) - (down >> bit & 1u ? INFINITY : 0.0f);

@@ -97,11 +97,12 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32
   if (marked) {      // some row does not see every key: what it does not see scores -inf, weight 0 below, whatever the reference
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int32_t from = r.low[n] - key0 - 8 * g, sinks = a.n_sink - key0 - 8 * g, upto = r.pos[n] - key0 - 8 * g;
+      const int32_t mine = key0 + 8 * anew(g), from = a.window > 0 ? r.low[n] - mine : -1, upto = r.pos[n] - mine;      // seen: from < key <= upto, and the first tokens
+      const uint32_t width = (uint32_t)max(upto - from, 0);
+      const int32_t sinks = a.window > 0 ? min(a.n_sink - mine, upto + 1) : -1;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][t][i] = 4 * t + i > upto || (a.window > 0 && 4 * t + i <= from && 4 * t + i >= sinks) ? -INFINITY : s[n][t][i];
+      for (int i = 0; i < 8; ++i) s[n][i / 4][i % 4] = (uint32_t)(i - 1 - from) < width || i < sinks ? s[n][i / 4][i % 4] : -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   x8<T> p[NT];
@@ -133,10 +134,11 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32
     }
     r.sum[n] += sum;
   }
+  const int at = anew(v_at<DP>(8 * g + (i16 >> 2), (i16 & 3) >> 1));      // v_at(.., 2 t + ..) is at ^ 2 t
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t) {
-    const int key = 8 * g + (i16 >> 2), c8 = 2 * t + ((i16 & 3) >> 1);
-    const u32x4 v = read_values(&lds[v_at<DP>(key, c8)], &lds[v_at<DP>(key + 4, c8)], i16 & 1);
+    const u32x4* row = lds + (at ^ 2 * t);
+    const u32x4 v = read_values(row, row + 4 * kRow<DP>, i16 & 1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) r.o[n][t] = mfma(__builtin_bit_cast(x8<T>, v), p[n], r.o[n][t]);
   }
@@ -255,6 +257,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
   KeyRows<T, F8, DP> kr;
   V values;
   u32x4* lds = s_tile[wave];
+  bool bad = false;
   while (sh.at < sh.end) {
     const int b = sh.b, kvh = sh.kvh;
     const int32_t take = (int32_t)min((int64_t)(sh.units - sh.unit), sh.end - sh.at);
@@ -289,68 +292,65 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
 #pragma unroll
       for (int t = 0; t < DP / 16; ++t) r.o[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    // pages of a tile's first and 17th key (the tile's end may lie beyond the request's)
-    auto pages_at = [&](int32_t v, int32_t* page) {
-      const int32_t key0 = tile_of(keys, v) * KT;
-      page[0] = page_of_all(a, b, key0);
-      page[1] = page_of_all(a, b, min(key0 + 16, q.len - 1));
+    // where the first and the second 16 keys of a tile begin in the cache, in bytes (the tile's end may lie beyond the request's)
+    auto find = [&](int32_t v, int64_t* at) {
+      const int32_t key0 = tile_of(keys, v) * KT, key1 = min(key0 + 16, q.len - 1);
+      at[0] = row_at(a, kvh, key0, page_of_all(a, b, key0, &bad), row_bytes);
+      at[1] = row_at(a, kvh, key1, page_of_all(a, b, key1, &bad), row_bytes);
     };
-    // this lane's rows of K, and the values' rows, of tile v
-    auto load_keys = [&](int32_t v, const int32_t* page) {
+    auto load_keys = [&](int32_t v, const int64_t* at) {
       const int32_t key0 = tile_of(keys, v) * KT;
-      const char* at[2];
+      const char* row[2];
       if (by_sixteen(a, key0, KT, q.len)) {
-        const char* lo = (const char*)a.k_cache + row_at(a, kvh, key0, page[0], row_bytes);
-        const char* hi = (const char*)a.k_cache + row_at(a, kvh, key0 + 16, page[1], row_bytes);
+        const char* from = (const char*)a.k_cache + (n16 < 8 ? at[0] : at[1]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) at[t] = (n16 < 8 ? lo : hi) + (key_of_row(t, n16) & 15) * row_bytes;
+        for (int t = 0; t < 2; ++t) row[t] = from + (key_of_row(t, n16) & 15) * row_bytes;
       } else {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const int32_t key = min(key0 + key_of_row(t, n16), q.len - 1);
-          at[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes);
+          const int32_t key = min(key0 + key_of_row(t, anew(n16)), q.len - 1);
+          row[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key, &bad), row_bytes);
         }
       }
-      kr.load(at, row_bytes);
+      kr.load(row, row_bytes);
     };
-    auto load_values = [&](int32_t v, const int32_t* page) {
+    auto load_values = [&](int32_t v, const int64_t* at) {
       const int32_t key0 = tile_of(keys, v) * KT;
-      const int c = lane % V::kPerRow * 16, off = c < row_bytes ? c : 0;
       if (by_sixteen(a, key0, KT, q.len)) {
-        const char* lo = (const char*)a.v_cache + row_at(a, kvh, key0, page[0], row_bytes);
-        const char* hi = (const char*)a.v_cache + row_at(a, kvh, key0 + 16, page[1], row_bytes);
-        const uint32_t mine = lane / V::kPerRow * row_bytes + off;
+        const int c = lane % V::kPerRow * 16;
+        const uint32_t mine = lane / V::kPerRow * row_bytes + (c < row_bytes ? c : 0);
 #pragma unroll
         for (int i = 0; i < V::kEach; ++i) {
-          const int row = i * V::kRows;
-          values.x[i] = *(const u32x4*)((row < 16 ? lo : hi) + (row & 15) * row_bytes + mine);
+          const int first = i * V::kRows;
+          values.x[i] = *(const u32x4*)((const char*)a.v_cache + (first < 16 ? at[0] : at[1]) + (first & 15) * row_bytes + mine);
         }
       } else {
+        const int l = anew(lane), c = l % V::kPerRow * 16, off = c < row_bytes ? c : 0;
 #pragma unroll
         for (int i = 0; i < V::kEach; ++i) {
-          const int32_t key = min(key0 + lane / V::kPerRow + i * V::kRows, q.len - 1);
-          values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes) + off);
+          const int32_t key = min(key0 + l / V::kPerRow + i * V::kRows, q.len - 1);
+          values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key, &bad), row_bytes) + off);
         }
       }
     };
     int32_t v = v0 + wave;
     if (v < v1) {
-      int32_t page[2];
-      pages_at(v, page);
-      load_keys(v, page);
-      load_values(v, page);
-      if (v + 4 < v1) pages_at(v + 4, page);
+      int64_t next[2];
+      find(v, next);
+      load_keys(v, next);
+      load_values(v, next);
+      if (v + 4 < v1) find(v + 4, next);
       for (; v < v1; v += 4) {
         const int32_t key0 = tile_of(keys, v) * KT;
         const bool marked = hides<KT>(a, r.first, r.last, key0);
         f32x4 s[NT][2];
         kr.scores(row_bytes, r, s);
         __builtin_amdgcn_sched_barrier(0);     // what is loaded next takes the registers that are free now, not others
-        if (v + 4 < v1) load_keys(v + 4, page);
+        if (v + 4 < v1) load_keys(v + 4, next);
         values.write(lds, marked, (uint8_t*)s_marks[wave]);
         if (v + 4 < v1) {
-          load_values(v + 4, page);
-          if (v + 8 < v1) pages_at(v + 8, page);
+          load_values(v + 4, next);
+          if (v + 8 < v1) find(v + 8, next);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -418,6 +418,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
       if (sh.b >= a.n_req) break;
     }
   }
+  report(a, bad);
 }
 
 // Joins the pieces of the pairs that were cut: a block for each row of the pair that goes on beyond attend_narrow_kernel's block x.  The waves take the pieces in turn; the

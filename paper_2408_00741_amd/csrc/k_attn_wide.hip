@@ -9,8 +9,8 @@ __device__ __forceinline__ f32x16 mfma(x8<_Float16> a, x8<_Float16> b, f32x16 c)
 constexpr int KT = DYN_ATTN_KEYS_WIDE;
 
 // Where 8 elements (16 bytes) of a tile lie in LDS, in units of 16 bytes: rows one after the other, the position in the row turned by the row so that the
-// 16 lanes of a read hit all 64 banks: 16 keys' same elements of K, 4 keys' 32 neighbouring elements of V.
-// (Heads of 96 have the rows of 128.)
+// 16 lanes of a read hit all 64 banks: 16 keys' same elements of K, 4 keys' 32 neighbouring elements of V.  (Heads of 96 have the rows of 128.)  A step of the
+// products then changes bits of the position that the key does not add to: one exclusive or makes its address.
 template <int DP>
 constexpr int kRow = DP <= 64 ? 8 : 16;
 template <int DP>
@@ -39,12 +39,12 @@ __device__ __forceinline__ int swap23(int n) { return (n & 0x13) | ((n & 4) << 1
 template <typename T, int DP>
 __device__ __forceinline__ void scores(const Rows<T, DP>& r, const u32x4* lds_k, f32x16* s) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int at = anew(k_at<DP>(swap23(lane & 31), h));      // k_at(32 mt + .., 2 d + h) is (at ^ 2 d) + 32 mt rows
 #pragma unroll
   for (int mt = 0; mt < KT / 32; ++mt) {
-    const int key = 32 * mt + swap23(lane & 31);
     f32x16 acc = {};
 #pragma unroll
-    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, lds_k[k_at<DP>(key, 2 * d + h)]), r.q[d], acc);
+    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, lds_k[(at ^ 2 * d) + 32 * mt * kRow<DP>]), r.q[d], acc);
     s[mt] = acc;
   }
 }
@@ -54,24 +54,19 @@ __device__ __forceinline__ void scores(const Rows<T, DP>& r, const u32x4* lds_k,
 template <typename T, int DP>
 __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16* s, const u32x4* lds_v, bool marked, const uint32_t* marks, int32_t key0) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
-  const bool some_hidden = hides<KT>(a, r.first, r.last, key0);
   // register i of s[mt] is key 32 mt + 16 (i / 8) + 8 h + i % 8.  What a row does not see scores -inf: weight 0 below, whatever the reference.
-  if (some_hidden) {
-    const int32_t from = r.low - key0 - 8 * h, sinks = a.n_sink - key0 - 8 * h, upto = r.pos - key0 - 8 * h;
-    if (a.window > 0) {
+  if (marked && hides<KT>(a, r.first, r.last, key0)) {
+    const int32_t mine = key0 + 8 * anew(h), from = a.window > 0 ? r.low - mine : -1, upto = r.pos - mine;      // seen: from < key <= upto, and the first tokens
+    const uint32_t width = (uint32_t)max(upto - from, 0);
+    const int32_t sinks = a.window > 0 ? min(a.n_sink - mine, upto + 1) : -1;
 #pragma unroll
-      for (int mt = 0; mt < KT / 32; ++mt)
+    for (int mt = 0; mt < KT / 32; ++mt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int32_t at = 32 * mt + 16 * (i / 8) + i % 8;
-          s[mt][i] = at > upto || (at <= from && at >= sinks) ? -INFINITY : s[mt][i];
-        }
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < KT / 32; ++mt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[mt][i] = 32 * mt + 16 * (i / 8) + i % 8 > upto ? -INFINITY : s[mt][i];
-    }
+      for (int i = 0; i < 16; ++i) {
+        const int32_t at = 32 * mt + 16 * (i / 8) + i % 8;
+        s[mt][i] = (uint32_t)(at - 1 - from) < width || at < sinks ? s[mt][i] : -INFINITY;
+        if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+      }
   }
   float top = -INFINITY;
 #pragma unroll
@@ -105,14 +100,14 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16*
 
   // V^T: lane group lane / 16 has elements 16 (group % 2) + .. of keys 8 (group / 2) + ..
   const int g16 = lane >> 4, i16 = lane & 15;
-  auto value = [&](int st, int t) {
-    const int key = 16 * st + 8 * (g16 >> 1) + (i16 >> 2), c8 = 4 * t + 2 * (g16 & 1) + ((i16 & 3) >> 1);
-    return read_values(&lds_v[v_at<DP>(key, c8)], &lds_v[v_at<DP>(key + 4, c8)], i16 & 1);
-  };
+  const int at = anew(v_at<DP>(8 * (g16 >> 1) + (i16 >> 2), 2 * (g16 & 1) + ((i16 & 3) >> 1)));      // v_at(16 st + .., 4 t + ..) is (at ^ 4 t) + 16 st rows
 #pragma unroll
   for (int st = 0; st < KT / 16; ++st)
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) r.o[t] = mfma(__builtin_bit_cast(x8<T>, value(st, t)), p[st], r.o[t]);
+    for (int t = 0; t < DP / 32; ++t) {
+      const u32x4* v = lds_v + (at ^ 4 * t) + 16 * st * kRow<DP>;
+      r.o[t] = mfma(__builtin_bit_cast(x8<T>, read_values(v, v + 4 * kRow<DP>, i16 & 1)), p[st], r.o[t]);
+    }
   // values that are not finite were taken out and marked: they go to the rows that see their keys.
   if (marked) {
     uint32_t any = 0;
@@ -166,18 +161,21 @@ struct Stage {
   static_assert(kRows <= 16 && KT * kPerRow % LANES == 0, "pieces");
   u32x4 x[kEach];
   static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kRows + i * (LANES / kPerRow); }
-  // `page`: of the pieces' rows.  Keys beyond the request's last one are read as the last one (no row sees them), pieces beyond the head's end as its first.
-  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, const int32_t* page) {
-    const int row_bytes = a.head_dim * (F8 ? 1 : 2), lane = threadIdx.x & 63, c = lane % kPerRow * 16, off = c < row_bytes ? c : 0;
+  // `at`: where the pieces' first rows begin in the cache (by_sixteen), in bytes.  Keys beyond the request's last one are read as the last one (no row sees
+  // them), pieces beyond the head's end as its first.
+  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, const int64_t* at, bool* bad) {
+    const int row_bytes = a.head_dim * (F8 ? 1 : 2), lane = threadIdx.x & 63;
     if (by_sixteen(a, key0, KT, len)) {
-      const uint32_t mine = lane / kPerRow * row_bytes + off;
+      const int c = lane % kPerRow * 16;
+      const uint32_t mine = lane / kPerRow * row_bytes + (c < row_bytes ? c : 0);
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key0 + first_row(wave, i), page[i], row_bytes) + mine);
+      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + at[i] + mine);
     } else {
+      const int l = anew(lane), c = l % kPerRow * 16, off = c < row_bytes ? c : 0;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int32_t key = min(key0 + first_row(wave, i) + lane / kPerRow, len - 1);
-        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key), row_bytes) + off);
+        const int32_t key = min(key0 + first_row(wave, i) + l / kPerRow, len - 1);
+        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad), row_bytes) + off);
       }
     }
   }
@@ -242,15 +240,20 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
   if (idle) r.last = -1;
   using S = Stage<T, F8, DP, 64 * NW>;
   S sk, sv;
+  bool bad = false;
+  const int row_bytes = a.head_dim * (F8 ? 1 : 2);
   if (v0 < v1) {
-    int32_t page[S::kEach];       // of this wave's pieces of the next tile
-    auto pages_at = [&](int32_t v) {
+    int64_t next[S::kEach];       // where this wave's pieces of the next tile begin
+    auto find = [&](int32_t v) {
 #pragma unroll
-      for (int i = 0; i < S::kEach; ++i) page[i] = page_of_all(a, b, min(tile_of(keys, v) * KT + S::first_row(wave, i), q.len - 1));
+      for (int i = 0; i < S::kEach; ++i) {
+        const int32_t key = min(tile_of(keys, v) * KT + S::first_row(wave, i), q.len - 1);
+        next[i] = row_at(a, kvh, key, page_of_all(a, b, key, &bad), row_bytes);
+      }
     };
     auto load = [&](int32_t v) {
-      sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, page);
-      sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, page);
+      sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+      sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
     };
     auto marked = [&](int32_t v) { return hides<KT>(a, first, last, tile_of(keys, v) * KT); };
     auto write = [&](int32_t v) {
@@ -258,9 +261,9 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
       sk.write_keys(a, at, wave);
       sv.write_values(at + kTile, marked(v), (uint8_t*)s_marks[(v - v0) & 1], wave);
     };
-    pages_at(v0);
+    find(v0);
     load(v0);
-    if (v0 + 1 < v1) pages_at(v0 + 1);
+    if (v0 + 1 < v1) find(v0 + 1);
     write(v0);
     __syncthreads();
     for (int32_t v = v0; v < v1; ++v) {
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
       const int32_t key0 = tile_of(keys, v) * KT;
       if (v + 1 < v1) {
         load(v + 1);
-        if (v + 2 < v1) pages_at(v + 2);
+        if (v + 2 < v1) find(v + 2);
       }
       // none of this wave's rows sees a key of the tile: beyond the last row's, or before the first row's window and after the first tokens
       if (key0 <= r.last && !(a.window > 0 && key0 + KT - 1 <= r.first - a.window && key0 >= a.n_sink)) {
@@ -280,6 +283,7 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
       __syncthreads();
     }
   }
+  report(a, bad);
   const int32_t row = base + 32 * wave + (lane & 31);
   const int h = lane >> 5;
   const float sum = r.sum + __shfl_xor(r.sum, 32);
