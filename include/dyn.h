@@ -484,7 +484,7 @@ int dyn_hierarchy(dyn_profile* profile, const dyn_trace_view* coarse, const dyn_
  * x % page_tokens; its slot is page * page_tokens + row.  The new tokens of all requests lie one
  * request after the other: request b has tokens cu_new[b] .. cu_new[b+1]-1.
  * Limits: page_tokens a power of two up to 4096, n_page * page_tokens < 2^31,
- * n_req * max_pages < 2^31, n_q_head a multiple of n_kv_head, head_dim a multiple of 16 up to
+ * n_req * max_pages < 2^31, a page of all heads below 2^31 bytes, n_q_head a multiple of n_kv_head, head_dim a multiple of 16 up to
  * 128.  These calls need no profile handle; they may be captured into a HIP graph.        */
 #define DYN_T_F16 1
 #define DYN_T_BF16 2

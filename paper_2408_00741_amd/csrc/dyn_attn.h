@@ -170,10 +170,10 @@ __device__ __forceinline__ int32_t inside(const AttnArgs& a, int32_t entry, bool
 __device__ __forceinline__ int32_t page_of(const AttnArgs& a, int b, int32_t key, bool* bad) {
   return inside(a, a.table[(size_t)b * a.max_pages + (key >> a.page_shift)], bad);
 }
-// The same for a key that is the same in all lanes: a scalar load, which waits for none of the vector loads in flight.
-__device__ __forceinline__ int32_t page_of_all(const AttnArgs& a, int b, int32_t key, bool* bad) {
+// The table's entry for a key that is the same in all lanes: a scalar load, which waits for none of the vector loads in flight.
+__device__ __forceinline__ int32_t entry_of_all(const AttnArgs& a, int b, int32_t key) {
   typedef const __attribute__((address_space(4))) int32_t* constant;
-  return inside(a, ((constant)a.table)[(size_t)b * a.max_pages + (key >> a.page_shift)], bad);
+  return ((constant)a.table)[(size_t)b * a.max_pages + (key >> a.page_shift)];
 }
 __device__ __forceinline__ void report(const AttnArgs& a, bool bad) {
   if (bad) atomicOr(&a.header->status, DYN_WS_BAD_PAGE);
@@ -182,8 +182,8 @@ __device__ __forceinline__ void report(const AttnArgs& a, bool bad) {
 __device__ __forceinline__ bool by_sixteen(const AttnArgs& a, int32_t key0, int keys, int32_t len) { return a.page_shift >= 4 && key0 + keys <= len; }
 
 // Where a key's row begins in the cache, in bytes; `page`: the key's.
-__device__ __forceinline__ int64_t row_at(const AttnArgs& a, int kvh, int32_t key, int32_t page, int row_bytes) {
-  return ((((int64_t)page * a.n_kv_head + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * row_bytes;
+__device__ __forceinline__ int64_t row_at(const AttnArgs& a, int kvh, int32_t key, int32_t page) {
+  return (int64_t)((uint64_t)(uint32_t)page * a.page_bytes) + (((uint32_t)kvh << a.page_shift) + (uint32_t)(key & ((1 << a.page_shift) - 1))) * a.row_bytes;
 }
 
 // 8 values on their way to LDS.  Those that are not finite are taken out and marked, a bit for +inf (`up`) and one for -inf (`down`), both for what is not a
@@ -208,6 +208,14 @@ __device__ __forceinline__ u32x4 take_out(u32x4 x, uint8_t* up_to, uint8_t* down
 __device__ __forceinline__ int anew(int x) {
   asm volatile("" : "+v"(x));
   return x;
+}
+
+// The greater of this lane's value and that of the lane 32 away.  In assembly: of the builtin's two results for equal operands the compiler keeps one, which is the
+// other lane's in half of the lanes.
+__device__ __forceinline__ float max_across_32(float x) {
+  float y = x;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+  return fmaxf(x, y);
 }
 
 // What two marks are worth; both: not a number.

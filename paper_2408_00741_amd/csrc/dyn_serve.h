@@ -34,6 +34,7 @@ struct AttnArgs {
   const void* k_cache; const void* v_cache; const float* k_scale; const float* v_scale;
   const int32_t* table; const int32_t* cu; const int32_t* kv_len;
   int32_t n_req, n_token, n_kv_head, group, head_dim, page_shift, n_page, max_pages, window, n_sink;
+  uint32_t row_bytes, page_bytes; // of a key's row of one head, of a page with all heads
   float scale;
   int32_t type, cache_type;
   bool q_vec, o_vec;              // 16-byte loads of queries, 8-byte stores of outputs are aligned

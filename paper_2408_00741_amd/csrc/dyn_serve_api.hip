@@ -187,6 +187,8 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   if ((int64_t)p->n_req * p->max_pages >= ((int64_t)1 << 31) || ((int64_t)p->max_pages << shift) >= ((int64_t)1 << 31)) { dyn_set_error("n_req * max_pages and max_pages * page_tokens must stay below 2^31"); return DYN_E_SHAPE; }
   const int64_t group = p->n_q_head / p->n_kv_head;
   if ((int64_t)p->n_token * group >= ((int64_t)1 << 31) || ((int64_t)p->n_token * group / (32 * DYN_ATTN_WAVES_WIDE) + p->n_req) * p->n_kv_head >= ((int64_t)1 << 31)) { dyn_set_error("too many rows"); return DYN_E_SHAPE; }
+  const int64_t row_bytes = p->head_dim * (p->cache_type == DYN_T_E4M3 ? 1 : 2), page_bytes = ((int64_t)p->n_kv_head << shift) * row_bytes;
+  if (page_bytes >= ((int64_t)1 << 31)) { dyn_set_error("a page must stay below 2^31 bytes"); return DYN_E_SHAPE; }
   if (p->window < 0 || p->n_sink < 0) { dyn_set_error("window or n_sink < 0"); return DYN_E_RANGE; }
   if (!isfinite(p->scale)) { dyn_set_error("scale is not finite"); return DYN_E_NOTFINITE; }
   if ((p->k_scale || p->v_scale) && p->cache_type != DYN_T_E4M3) { dyn_set_error("scales belong to an 8-bit cache"); return DYN_E_RANGE; }
@@ -202,6 +204,7 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.table = p->block_table; a.cu = p->cu_new; a.kv_len = p->kv_len;
   a.n_req = p->n_req; a.n_token = p->n_token; a.n_kv_head = p->n_kv_head; a.group = (int32_t)group; a.head_dim = p->head_dim;
   a.page_shift = shift; a.n_page = p->n_page; a.max_pages = p->max_pages; a.window = p->window; a.n_sink = p->n_sink;
+  a.row_bytes = (uint32_t)row_bytes; a.page_bytes = (uint32_t)page_bytes;
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
   a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow; a.rows_most = s.rows_most;
   a.blocks_narrow = s.blocks_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;

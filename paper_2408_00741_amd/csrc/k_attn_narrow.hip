@@ -292,11 +292,18 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
 #pragma unroll
       for (int t = 0; t < DP / 16; ++t) r.o[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    // where the first and the second 16 keys of a tile begin in the cache, in bytes (the tile's end may lie beyond the request's)
+    // where the first and the second 16 keys of a tile begin in the cache, in bytes (the tile's end may lie beyond the request's); the table's entries
+    // are fetched a tile before
+    int32_t entry[2];
+    auto fetch = [&](int32_t v) {
+      const int32_t key0 = tile_of(keys, min(v, v1 - 1)) * KT;
+      entry[0] = entry_of_all(a, b, key0);
+      entry[1] = entry_of_all(a, b, min(key0 + 16, q.len - 1));
+    };
     auto find = [&](int32_t v, int64_t* at) {
-      const int32_t key0 = tile_of(keys, v) * KT, key1 = min(key0 + 16, q.len - 1);
-      at[0] = row_at(a, kvh, key0, page_of_all(a, b, key0, &bad), row_bytes);
-      at[1] = row_at(a, kvh, key1, page_of_all(a, b, key1, &bad), row_bytes);
+      const int32_t key0 = tile_of(keys, min(v, v1 - 1)) * KT;
+      at[0] = row_at(a, kvh, key0, inside(a, entry[0], &bad));
+      at[1] = row_at(a, kvh, min(key0 + 16, q.len - 1), inside(a, entry[1], &bad));
     };
     auto load_keys = [&](int32_t v, const int64_t* at) {
       const int32_t key0 = tile_of(keys, v) * KT;
@@ -309,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int32_t key = min(key0 + key_of_row(t, anew(n16)), q.len - 1);
-          row[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key, &bad), row_bytes);
+          row[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key, &bad));
         }
       }
       kr.load(row, row_bytes);
@@ -329,28 +336,32 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < V::kEach; ++i) {
           const int32_t key = min(key0 + l / V::kPerRow + i * V::kRows, q.len - 1);
-          values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key, &bad), row_bytes) + off);
+          values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key, &bad)) + off);
         }
       }
     };
     int32_t v = v0 + wave;
     if (v < v1) {
       int64_t next[2];
+      fetch(v);
       find(v, next);
+      fetch(v + 4);
       load_keys(v, next);
       load_values(v, next);
-      if (v + 4 < v1) find(v + 4, next);
       for (; v < v1; v += 4) {
         const int32_t key0 = tile_of(keys, v) * KT;
         const bool marked = hides<KT>(a, r.first, r.last, key0);
         f32x4 s[NT][2];
         kr.scores(row_bytes, r, s);
         __builtin_amdgcn_sched_barrier(0);     // what is loaded next takes the registers that are free now, not others
-        if (v + 4 < v1) load_keys(v + 4, next);
+        if (v + 4 < v1) {
+          find(v + 4, next);
+          fetch(v + 8);
+          load_keys(v + 4, next);
+        }
         values.write(lds, marked, (uint8_t*)s_marks[wave]);
         if (v + 4 < v1) {
           load_values(v + 4, next);
-          if (v + 8 < v1) find(v + 8, next);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -175,7 +175,7 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int32_t key = min(key0 + first_row(wave, i) + l / kPerRow, len - 1);
-        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad), row_bytes) + off);
+        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad)) + off);
       }
     }
   }
@@ -210,9 +210,48 @@ struct Stage {
   }
 };
 
+// The same straight into LDS, for 16-bit heads that fill their rows (64, 96 or 128 wide): no registers, no second way.  A load puts its 64 lanes' pieces one after the other,
+// so that a lane takes the piece of its row that belongs where it writes.
+template <typename T, int DP, int LANES>
+struct Direct {
+  static constexpr int kPerRow = kRow<DP>, kRows = 64 / kPerRow, kEach = KT * kPerRow / LANES;
+  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kRows + i * (LANES / kPerRow); }
+  // the place in its row of the piece of lane `lane` (all of a wave's pieces have it at the same place: their first rows are multiples of 16 apart)
+  static __device__ __forceinline__ int key_piece(int wave, int lane) { return k_at<DP>(first_row(wave, 0) + lane / kPerRow, lane % kPerRow) % kPerRow; }
+  static __device__ __forceinline__ int value_piece(int wave, int lane) { return v_at<DP>(first_row(wave, 0) + lane / kPerRow, lane % kPerRow) % kPerRow; }
+  static __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, u32x4* lds, int piece, int kvh, int b, int32_t key0, int32_t len, int wave, const int64_t* at, bool* bad) {
+    typedef const __attribute__((address_space(1))) uint32_t* from;
+    typedef __attribute__((address_space(3))) uint32_t* to;
+    const int lane = threadIdx.x & 63;
+    if (piece * 8 >= DP) return;             // heads of 96: the rest of the row is not read
+    if (by_sixteen(a, key0, KT, len)) {
+      const uint32_t mine = lane / kPerRow * (DP * 2) + piece * 16;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) __builtin_amdgcn_global_load_lds((from)((const char*)cache + at[i] + mine), (to)(lds + first_row(wave, i) * kPerRow), 16, 0, 0);
+    } else {
+      const int l = anew(lane);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int32_t key = min(key0 + first_row(wave, i) + l / kPerRow, len - 1);
+        __builtin_amdgcn_global_load_lds((from)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad)) + piece * 16), (to)(lds + first_row(wave, i) * kPerRow), 16, 0, 0);
+      }
+    }
+  }
+  // Takes the values that are not finite out of a tile in LDS.
+  static __device__ __forceinline__ void mark_values(u32x4* lds, uint8_t* marks, int wave) {
+    const int lane = anew(threadIdx.x & 63), c = value_piece(wave, lane);
+    if (c * 8 >= DP) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int row = first_row(wave, i) + lane / kPerRow, at = first_row(wave, i) * kPerRow + lane;
+      lds[at] = take_out<T>(lds[at], marks + row * (DP / 8) + c, marks + (KT + row) * (DP / 8) + c);
+    }
+  }
+};
+
 // Requests of more rows: a block has 32 rows for each of its waves, all waves read the same tiles of 64 keys from LDS, two tiles in turn, the next
 // one's loads in flight while one is worked on.  Bound by the matrix instructions and the exponentials beside them.
-template <typename T, bool F8, int DP>
+template <typename T, bool F8, int DP, bool DIRECT>
 __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kernel(AttnArgs a) {
   constexpr int NW = DYN_ATTN_WAVES_WIDE, R = 32 * NW, kTile = KT * kRow<DP>;   // 16-byte pieces of K (or V) of a tile
   __shared__ u32x4 s_tile[2][2 * kTile];
@@ -239,48 +278,83 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
   load_rows<T, DP>(a, q, kvh, idle ? 0 : base + 32 * wave, idle ? 0 : rows, r);
   if (idle) r.last = -1;
   using S = Stage<T, F8, DP, 64 * NW>;
-  S sk, sv;
   bool bad = false;
-  const int row_bytes = a.head_dim * (F8 ? 1 : 2);
   if (v0 < v1) {
-    int64_t next[S::kEach];       // where this wave's pieces of the next tile begin
+    // where this wave's pieces of the next tile begin; the table's entries are fetched a tile before
+    int64_t next[S::kEach];
+    int32_t entry[S::kEach];
+    auto key_at = [&](int32_t v, int i) { return min(tile_of(keys, min(v, v1 - 1)) * KT + S::first_row(wave, i), q.len - 1); };
+    auto fetch = [&](int32_t v) {
+#pragma unroll
+      for (int i = 0; i < S::kEach; ++i) entry[i] = entry_of_all(a, b, key_at(v, i));
+    };
     auto find = [&](int32_t v) {
 #pragma unroll
-      for (int i = 0; i < S::kEach; ++i) {
-        const int32_t key = min(tile_of(keys, v) * KT + S::first_row(wave, i), q.len - 1);
-        next[i] = row_at(a, kvh, key, page_of_all(a, b, key, &bad), row_bytes);
-      }
-    };
-    auto load = [&](int32_t v) {
-      sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-      sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+      for (int i = 0; i < S::kEach; ++i) next[i] = row_at(a, kvh, key_at(v, i), inside(a, entry[i], &bad));
     };
     auto marked = [&](int32_t v) { return hides<KT>(a, first, last, tile_of(keys, v) * KT); };
-    auto write = [&](int32_t v) {
-      u32x4* at = s_tile[(v - v0) & 1];
-      sk.write_keys(a, at, wave);
-      sv.write_values(at + kTile, marked(v), (uint8_t*)s_marks[(v - v0) & 1], wave);
-    };
-    find(v0);
-    load(v0);
-    if (v0 + 1 < v1) find(v0 + 1);
-    write(v0);
-    __syncthreads();
-    for (int32_t v = v0; v < v1; ++v) {
+    auto work = [&](int32_t v) {
       const u32x4* at = s_tile[(v - v0) & 1];
       const int32_t key0 = tile_of(keys, v) * KT;
-      if (v + 1 < v1) {
-        load(v + 1);
-        if (v + 2 < v1) find(v + 2);
-      }
       // none of this wave's rows sees a key of the tile: beyond the last row's, or before the first row's window and after the first tokens
       if (key0 <= r.last && !(a.window > 0 && key0 + KT - 1 <= r.first - a.window && key0 >= a.n_sink)) {
         f32x16 s[KT / 32];
         scores<T, DP>(r, at, s);
         weigh<T, DP>(a, r, s, at + kTile, marked(v), s_marks[(v - v0) & 1], key0);
       }
-      if (v + 1 < v1) write(v + 1);
+    };
+    if constexpr (DIRECT) {
+      using D = Direct<T, DP, 64 * NW>;
+      const int key_piece = D::key_piece(wave, lane), value_piece = D::value_piece(wave, lane);
+      auto load = [&](int32_t v) {
+        u32x4* at = s_tile[(v - v0) & 1];
+        D::load(a, a.k_cache, at, key_piece, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+        D::load(a, a.v_cache, at + kTile, value_piece, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+      };
+      fetch(v0);
+      find(v0);
+      fetch(v0 + 1);
+      load(v0);
+      for (int32_t v = v0; v < v1; ++v) {
+        __syncthreads();           // this tile is there, and all waves are through with the one before
+        if (marked(v)) {
+          D::mark_values(s_tile[(v - v0) & 1] + kTile, (uint8_t*)s_marks[(v - v0) & 1], wave);
+          __syncthreads();
+        }
+        if (v + 1 < v1) {
+          find(v + 1);
+          fetch(v + 2);
+          load(v + 1);
+        }
+        work(v);
+      }
+    } else {
+      S sk, sv;
+      auto load = [&](int32_t v) {
+        sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+        sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+      };
+      auto write = [&](int32_t v) {
+        u32x4* at = s_tile[(v - v0) & 1];
+        sk.write_keys(a, at, wave);
+        sv.write_values(at + kTile, marked(v), (uint8_t*)s_marks[(v - v0) & 1], wave);
+      };
+      fetch(v0);
+      find(v0);
+      fetch(v0 + 1);
+      load(v0);
+      write(v0);
       __syncthreads();
+      for (int32_t v = v0; v < v1; ++v) {
+        if (v + 1 < v1) {
+          find(v + 1);
+          fetch(v + 2);
+          load(v + 1);
+        }
+        work(v);
+        if (v + 1 < v1) write(v + 1);
+        __syncthreads();
+      }
     }
   }
   report(a, bad);
@@ -323,7 +397,9 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
 
 template <typename T, bool F8, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attend_wide_kernel<T, F8, DP>), dim3((unsigned)a.n_tile_wide * a.n_kv_head, (unsigned)a.n_chunk_wide), dim3(64 * DYN_ATTN_WAVES_WIDE), 0, s, a);
+  const dim3 grid((unsigned)a.n_tile_wide * a.n_kv_head, (unsigned)a.n_chunk_wide), block(64 * DYN_ATTN_WAVES_WIDE);
+  if (!F8 && a.head_dim == DP) hipLaunchKernelGGL((attend_wide_kernel<T, F8, DP, !F8>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_wide_kernel<T, F8, DP, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 template <typename T, bool F8>
