@@ -225,10 +225,9 @@ __device__ __forceinline__ float marked_value(uint32_t up, uint32_t down, int bi
 
 // The left operand of the second product: 8 keys of one element, by two transposing reads of 4 keys each; lane i of 16 gives the address of key i / 4's elements
 // 4 (i % 4) .. and gets the 4 keys of element i.
-__device__ __forceinline__ u32x4 read_values(const u32x4* lo, const u32x4* hi, int half) {
+__device__ __forceinline__ u32x4 read_values(const __attribute__((address_space(3))) u32x4* lo, const __attribute__((address_space(3))) u32x4* hi) {
   typedef __attribute__((address_space(3))) s16x4* lds4;
-  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((const s16x4*)lo + half));
-  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((const s16x4*)hi + half));
+  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)hi);
   return __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 

@@ -134,11 +134,13 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32
     }
     r.sum[n] += sum;
   }
-  const int at = anew(v_at<DP>(8 * g + (i16 >> 2), (i16 & 3) >> 1));      // v_at(.., 2 t + ..) is at ^ 2 t
+  typedef const __attribute__((address_space(3))) u32x4* LdsRead;
+  // v_at(.., 2 t + ..) is (at ^ 32 t bytes): a wave's tile begins at a multiple of 256 bytes
+  const uint32_t at = anew(16 * v_at<DP>(8 * g + (i16 >> 2), (i16 & 3) >> 1) + 8 * (i16 & 1)) + (uint32_t)(uintptr_t)(LdsRead)lds;
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t) {
-    const u32x4* row = lds + (at ^ 2 * t);
-    const u32x4 v = read_values(row, row + 4 * kRow<DP>, i16 & 1);
+    const LdsRead row = (LdsRead)(uintptr_t)(at ^ 32 * t);
+    const u32x4 v = read_values(row, row + 4 * kRow<DP>);
 #pragma unroll
     for (int n = 0; n < NT; ++n) r.o[n][t] = mfma(__builtin_bit_cast(x8<T>, v), p[n], r.o[n][t]);
   }
@@ -245,7 +247,7 @@ __device__ __forceinline__ int64_t piece_row(const AttnArgs& a, int block, int s
 // are short (5.4).
 template <typename T, bool F8, int DP, int NT>
 __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
-  __shared__ u32x4 s_tile[4][KT * kRow<DP>];           // a wave's values, and at the end the sums of 16 rows
+  __shared__ __attribute__((aligned(256))) u32x4 s_tile[4][KT * kRow<DP>];           // a wave's values, and at the end the sums of 16 rows
   __shared__ uint32_t s_marks[4][2 * KT * DP / 32];
   __shared__ float s_m[4][16 * NT], s_sum[4][16 * NT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;

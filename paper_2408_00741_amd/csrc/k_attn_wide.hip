@@ -35,27 +35,31 @@ struct Rows {
 // Row n (of the first product's left operand) of 32 keys is key swap23(n): bits 2 and 3 swapped.
 __device__ __forceinline__ int swap23(int n) { return (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1); }
 
+// LDS by its byte address: the tiles begin at multiples of 256 bytes, so that the exclusive or of a step can be taken in the address itself.
+typedef const __attribute__((address_space(3))) u32x4* LdsRead;
+__device__ __forceinline__ uint32_t lds_address(const u32x4* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) u32x4*)p; }
+
 // S^T of a tile whose keys are in LDS.
 template <typename T, int DP>
 __device__ __forceinline__ void scores(const Rows<T, DP>& r, const u32x4* lds_k, f32x16* s) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
-  const int at = anew(k_at<DP>(swap23(lane & 31), h));      // k_at(32 mt + .., 2 d + h) is (at ^ 2 d) + 32 mt rows
+  const uint32_t at = anew(16 * k_at<DP>(swap23(lane & 31), h)) + lds_address(lds_k);      // k_at(32 mt + .., 2 d + h) is (at ^ 32 d bytes) + 32 mt rows
 #pragma unroll
   for (int mt = 0; mt < KT / 32; ++mt) {
     f32x16 acc = {};
 #pragma unroll
-    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, lds_k[(at ^ 2 * d) + 32 * mt * kRow<DP>]), r.q[d], acc);
+    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, ((LdsRead)(uintptr_t)(at ^ 32 * d))[32 * mt * kRow<DP>]), r.q[d], acc);
     s[mt] = acc;
   }
 }
 
-// The rest of a tile: from the scores to the weighted sum of the values in LDS (v_at).  `key0`: the first key's position; `marked`: `marks`
-// has two bits of every value (take_out).
+// The rest of a tile: from the scores to the weighted sum of the values in LDS (v_at).  `key0`: the first key's position; `hidden`: some row does
+// not see all of its keys; `marked`: `marks` has two bits of every value (take_out).
 template <typename T, int DP>
-__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16* s, const u32x4* lds_v, bool marked, const uint32_t* marks, int32_t key0) {
+__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16* s, const u32x4* lds_v, bool hidden, bool marked, const uint32_t* marks, int32_t key0) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
   // register i of s[mt] is key 32 mt + 16 (i / 8) + 8 h + i % 8.  What a row does not see scores -inf: weight 0 below, whatever the reference.
-  if (marked && hides<KT>(a, r.first, r.last, key0)) {
+  if (hidden) {
     const int32_t mine = key0 + 8 * anew(h), from = a.window > 0 ? r.low - mine : -1, upto = r.pos - mine;      // seen: from < key <= upto, and the first tokens
     const uint32_t width = (uint32_t)max(upto - from, 0);
     const int32_t sinks = a.window > 0 ? min(a.n_sink - mine, upto + 1) : -1;
@@ -73,7 +77,7 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16*
   for (int mt = 0; mt < KT / 32; ++mt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[mt][i]);
-  top = fmaxf(top, __shfl_xor(top, 32));
+  top = max_across_32(top);
   const bool raise = (top - r.m) * r.c > kRaise || (r.m == -INFINITY && top > -INFINITY);
   if (__any(raise)) {
     const float m = fmaxf(r.m, top);
@@ -100,13 +104,13 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16*
 
   // V^T: lane group lane / 16 has elements 16 (group % 2) + .. of keys 8 (group / 2) + ..
   const int g16 = lane >> 4, i16 = lane & 15;
-  const int at = anew(v_at<DP>(8 * (g16 >> 1) + (i16 >> 2), 2 * (g16 & 1) + ((i16 & 3) >> 1)));      // v_at(16 st + .., 4 t + ..) is (at ^ 4 t) + 16 st rows
+  const uint32_t at = anew(16 * v_at<DP>(8 * (g16 >> 1) + (i16 >> 2), 2 * (g16 & 1) + ((i16 & 3) >> 1)) + 8 * (i16 & 1)) + lds_address(lds_v);      // v_at(16 st + .., 4 t + ..) is (at ^ 64 t bytes) + 16 st rows
 #pragma unroll
   for (int st = 0; st < KT / 16; ++st)
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) {
-      const u32x4* v = lds_v + (at ^ 4 * t) + 16 * st * kRow<DP>;
-      r.o[t] = mfma(__builtin_bit_cast(x8<T>, read_values(v, v + 4 * kRow<DP>, i16 & 1)), p[st], r.o[t]);
+      const LdsRead v = (LdsRead)(uintptr_t)(at ^ 64 * t) + 16 * st * kRow<DP>;
+      r.o[t] = mfma(__builtin_bit_cast(x8<T>, read_values(v, v + 4 * kRow<DP>)), p[st], r.o[t]);
     }
   // values that are not finite were taken out and marked: they go to the rows that see their keys.
   if (marked) {
@@ -153,23 +157,24 @@ __device__ __forceinline__ void load_rows(const AttnArgs& a, const Request& q, i
   for (int t = 0; t < DP / 32; ++t) r.o[t] = f32x16{};
 }
 
-// The part of a tile of keys or values that a lane carries from the cache to LDS, in pieces of 16 bytes, whole rows by neighbouring lanes: a wave's piece i is
-// rows first_row(wave, i) .. of 64 / kPerRow.
-template <typename T, bool F8, int DP, int LANES>
+// The part of a tile of keys or values that a wave carries from the cache to LDS: 16 neighbouring rows, which lie in one page of 16 tokens and more; a lane has pieces of
+// 16 bytes, whole rows by neighbouring lanes.
+constexpr int kWaveRows = KT / DYN_ATTN_WAVES_WIDE;
+static_assert(kWaveRows == 16, "by_sixteen");
+template <typename T, bool F8, int DP>
 struct Stage {
-  static constexpr int kPerRow = F8 ? kRow<DP> / 2 : kRow<DP>, kRows = 64 / kPerRow, kEach = KT * kPerRow / LANES;
-  static_assert(kRows <= 16 && KT * kPerRow % LANES == 0, "pieces");
+  static constexpr int kPerRow = F8 ? kRow<DP> / 2 : kRow<DP>, kRows = 64 / kPerRow, kEach = kWaveRows / kRows;
   u32x4 x[kEach];
-  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kRows + i * (LANES / kPerRow); }
-  // `at`: where the pieces' first rows begin in the cache (by_sixteen), in bytes.  Keys beyond the request's last one are read as the last one (no row sees
+  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kWaveRows + i * kRows; }
+  // `at`: where the wave's first row begins in the cache (by_sixteen), in bytes.  Keys beyond the request's last one are read as the last one (no row sees
   // them), pieces beyond the head's end as its first.
-  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, const int64_t* at, bool* bad) {
+  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, int64_t at, bool* bad) {
     const int row_bytes = a.head_dim * (F8 ? 1 : 2), lane = threadIdx.x & 63;
     if (by_sixteen(a, key0, KT, len)) {
       const int c = lane % kPerRow * 16;
       const uint32_t mine = lane / kPerRow * row_bytes + (c < row_bytes ? c : 0);
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + at[i] + mine);
+      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + at + i * kRows * row_bytes + mine);
     } else {
       const int l = anew(lane), c = l % kPerRow * 16, off = c < row_bytes ? c : 0;
 #pragma unroll
@@ -212,38 +217,45 @@ struct Stage {
 
 // The same straight into LDS, for 16-bit heads that fill their rows (64, 96 or 128 wide): no registers, no second way.  A load puts its 64 lanes' pieces one after the other,
 // so that a lane takes the piece of its row that belongs where it writes.
-template <typename T, int DP, int LANES>
+template <typename T, int DP>
 struct Direct {
-  static constexpr int kPerRow = kRow<DP>, kRows = 64 / kPerRow, kEach = KT * kPerRow / LANES;
-  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kRows + i * (LANES / kPerRow); }
-  // the place in its row of the piece of lane `lane` (all of a wave's pieces have it at the same place: their first rows are multiples of 16 apart)
-  static __device__ __forceinline__ int key_piece(int wave, int lane) { return k_at<DP>(first_row(wave, 0) + lane / kPerRow, lane % kPerRow) % kPerRow; }
-  static __device__ __forceinline__ int value_piece(int wave, int lane) { return v_at<DP>(first_row(wave, 0) + lane / kPerRow, lane % kPerRow) % kPerRow; }
-  static __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, u32x4* lds, int piece, int kvh, int b, int32_t key0, int32_t len, int wave, const int64_t* at, bool* bad) {
+  static constexpr int kPerRow = kRow<DP>, kRows = 64 / kPerRow, kEach = kWaveRows / kRows;
+  // the piece of its row that lane `lane` takes of the wave's load i: of keys, of values (the same for all loads: their rows are multiples of 4 apart)
+  static __device__ __forceinline__ int key_piece(int i, int lane) { return k_at<DP>(i * kRows + lane / kPerRow, lane % kPerRow) % kPerRow; }
+  static __device__ __forceinline__ int value_piece(int lane) { return v_at<DP>(lane / kPerRow, lane % kPerRow) % kPerRow; }
+  template <bool KEYS>
+  static __device__ __forceinline__ void load(const AttnArgs& a, u32x4* lds, int kvh, int b, int32_t key0, int32_t len, int wave, int64_t at, bool* bad) {
     typedef const __attribute__((address_space(1))) uint32_t* from;
     typedef __attribute__((address_space(3))) uint32_t* to;
     const int lane = threadIdx.x & 63;
-    if (piece * 8 >= DP) return;             // heads of 96: the rest of the row is not read
+    const char* cache = (const char*)(KEYS ? a.k_cache : a.v_cache);
+    u32x4* here = lds + wave * kWaveRows * kPerRow;
     if (by_sixteen(a, key0, KT, len)) {
-      const uint32_t mine = lane / kPerRow * (DP * 2) + piece * 16;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) __builtin_amdgcn_global_load_lds((from)((const char*)cache + at[i] + mine), (to)(lds + first_row(wave, i) * kPerRow), 16, 0, 0);
+      for (int i = 0; i < kEach; ++i) {
+        const int piece = KEYS ? key_piece(i, lane) : value_piece(lane);
+        const uint32_t mine = (i * kRows + lane / kPerRow) * (DP * 2) + piece * 16;
+        if (kPerRow * 8 == DP || piece * 8 < DP)             // heads of 96: the rest of the row is not read
+          __builtin_amdgcn_global_load_lds((from)(cache + at + mine), (to)(here + i * 64), 16, 0, 0);
+      }
     } else {
       const int l = anew(lane);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int32_t key = min(key0 + first_row(wave, i) + l / kPerRow, len - 1);
-        __builtin_amdgcn_global_load_lds((from)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad)) + piece * 16), (to)(lds + first_row(wave, i) * kPerRow), 16, 0, 0);
+        const int piece = KEYS ? key_piece(i, l) : value_piece(l);
+        const int32_t key = min(key0 + wave * kWaveRows + i * kRows + l / kPerRow, len - 1);
+        const char* row = cache + row_at(a, kvh, key, page_of(a, b, key, bad));
+        if (kPerRow * 8 == DP || piece * 8 < DP) __builtin_amdgcn_global_load_lds((from)(row + piece * 16), (to)(here + i * 64), 16, 0, 0);
       }
     }
   }
   // Takes the values that are not finite out of a tile in LDS.
   static __device__ __forceinline__ void mark_values(u32x4* lds, uint8_t* marks, int wave) {
-    const int lane = anew(threadIdx.x & 63), c = value_piece(wave, lane);
+    const int lane = anew(threadIdx.x & 63), c = value_piece(lane);
     if (c * 8 >= DP) return;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int row = first_row(wave, i) + lane / kPerRow, at = first_row(wave, i) * kPerRow + lane;
+      const int row = wave * kWaveRows + i * kRows + lane / kPerRow, at = (wave * kWaveRows + i * kRows) * kPerRow + lane;
       lds[at] = take_out<T>(lds[at], marks + row * (DP / 8) + c, marks + (KT + row) * (DP / 8) + c);
     }
   }
@@ -254,7 +266,7 @@ struct Direct {
 template <typename T, bool F8, int DP, bool DIRECT>
 __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kernel(AttnArgs a) {
   constexpr int NW = DYN_ATTN_WAVES_WIDE, R = 32 * NW, kTile = KT * kRow<DP>;   // 16-byte pieces of K (or V) of a tile
-  __shared__ u32x4 s_tile[2][2 * kTile];
+  __shared__ __attribute__((aligned(256))) u32x4 s_tile[2][2 * kTile];
   __shared__ uint32_t s_marks[2][2 * KT * DP / 32];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.n_kv_head, chunk = blockIdx.y;
@@ -277,22 +289,25 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
   const bool idle = base + 32 * wave >= rows;
   load_rows<T, DP>(a, q, kvh, idle ? 0 : base + 32 * wave, idle ? 0 : rows, r);
   if (idle) r.last = -1;
-  using S = Stage<T, F8, DP, 64 * NW>;
   bool bad = false;
   if (v0 < v1) {
-    // where this wave's pieces of the next tile begin; the table's entries are fetched a tile before
-    int64_t next[S::kEach];
-    int32_t entry[S::kEach];
-    auto key_at = [&](int32_t v, int i) { return min(tile_of(keys, min(v, v1 - 1)) * KT + S::first_row(wave, i), q.len - 1); };
-    auto fetch = [&](int32_t v) {
-#pragma unroll
-      for (int i = 0; i < S::kEach; ++i) entry[i] = entry_of_all(a, b, key_at(v, i));
+    // where this wave's rows of the next tile begin; the table's entry is fetched a tile before
+    int64_t next = 0;
+    int32_t entry = 0;
+    auto key_at = [&](int32_t v) { return min(tile_of(keys, min(v, v1 - 1)) * KT + wave * kWaveRows, q.len - 1); };
+    auto fetch = [&](int32_t v) { entry = entry_of_all(a, b, key_at(v)); };
+    auto find = [&](int32_t v) { next = row_at(a, kvh, key_at(v), inside(a, entry, &bad)); };
+    // tiles [from, to) are seen in whole by all rows, of the block and of this wave (and others perhaps)
+    auto whole = [&](int32_t lo, int32_t hi, int32_t* from, int32_t* to) {
+      const int32_t shift = keys.first - keys.sink_tiles;              // of a tile's number and its keys, from the window on
+      *from = a.window > 0 && hi >= a.window ? max((hi - a.window) / KT + 1 - shift, keys.sink_tiles) : 0;
+      *to = max(lo + 1, 0) / KT - shift;
+      if (*to < keys.sink_tiles) *to = 0;                              // the window itself begins in the first tokens
     };
-    auto find = [&](int32_t v) {
-#pragma unroll
-      for (int i = 0; i < S::kEach; ++i) next[i] = row_at(a, kvh, key_at(v, i), inside(a, entry[i], &bad));
-    };
-    auto marked = [&](int32_t v) { return hides<KT>(a, first, last, tile_of(keys, v) * KT); };
+    int32_t block_from, block_to, wave_from, wave_to;
+    whole(first, last, &block_from, &block_to);
+    whole(r.first, r.last, &wave_from, &wave_to);
+    auto marked = [&](int32_t v) { return v < block_from || v >= block_to; };
     auto work = [&](int32_t v) {
       const u32x4* at = s_tile[(v - v0) & 1];
       const int32_t key0 = tile_of(keys, v) * KT;
@@ -300,16 +315,15 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
       if (key0 <= r.last && !(a.window > 0 && key0 + KT - 1 <= r.first - a.window && key0 >= a.n_sink)) {
         f32x16 s[KT / 32];
         scores<T, DP>(r, at, s);
-        weigh<T, DP>(a, r, s, at + kTile, marked(v), s_marks[(v - v0) & 1], key0);
+        weigh<T, DP>(a, r, s, at + kTile, v < wave_from || v >= wave_to, marked(v), s_marks[(v - v0) & 1], key0);
       }
     };
     if constexpr (DIRECT) {
-      using D = Direct<T, DP, 64 * NW>;
-      const int key_piece = D::key_piece(wave, lane), value_piece = D::value_piece(wave, lane);
+      using D = Direct<T, DP>;
       auto load = [&](int32_t v) {
         u32x4* at = s_tile[(v - v0) & 1];
-        D::load(a, a.k_cache, at, key_piece, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-        D::load(a, a.v_cache, at + kTile, value_piece, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+        D::template load<true>(a, at, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
+        D::template load<false>(a, at + kTile, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
       };
       fetch(v0);
       find(v0);
@@ -329,7 +343,7 @@ __global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kerne
         work(v);
       }
     } else {
-      S sk, sv;
+      Stage<T, F8, DP> sk, sv;
       auto load = [&](int32_t v) {
         sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
         sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
