@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -214,15 +215,15 @@ _lib.dyn_hierarchy.argtypes = [_vp, C.POINTER(_TraceView), C.POINTER(_TraceView)
 _lib.dyn_kv_step_workspace.restype = _sz
 _lib.dyn_kv_step_workspace.argtypes = [_i32]
 _lib.dyn_kv_step.restype = C.c_int
-_lib.dyn_kv_step.argtypes = [C.POINTER(_KvRequests), C.POINTER(_KvPlan), _vp, _sz, _vp]
+_lib.dyn_kv_step.argtypes = [_vp, _vp, _vp, _sz, _vp]       # structs: by reference, or packed (_PACK)
 _lib.dyn_rope_frequencies.restype = C.c_int
 _lib.dyn_rope_frequencies.argtypes = [C.POINTER(_RopeDesc), _vp, C.POINTER(C.c_double)]
 _lib.dyn_rope_append.restype = C.c_int
-_lib.dyn_rope_append.argtypes = [C.POINTER(_Append), _vp]
+_lib.dyn_rope_append.argtypes = [_vp, _vp]
 _lib.dyn_paged_attention_workspace.restype = _sz
 _lib.dyn_paged_attention_workspace.argtypes = [_i32] * 7
 _lib.dyn_paged_attention.restype = C.c_int
-_lib.dyn_paged_attention.argtypes = [C.POINTER(_Attention), _vp, _sz, _vp]
+_lib.dyn_paged_attention.argtypes = [_vp, _vp, _sz, _vp]
 _lib.dyn_timing_enable.restype = C.c_int
 _lib.dyn_timing_enable.argtypes = [C.c_int, _i32]
 _lib.dyn_timing_reset.restype = C.c_int
@@ -743,60 +744,106 @@ def dyn_select_config(profile: Profile, space: Dict[str, torch.Tensor], n_window
 # ---- the serving step that a profile is measured on ------------------------------------------------------------
 
 _TYPES = {torch.float16: DYN_T_F16, torch.bfloat16: DYN_T_BF16, torch.float8_e4m3fn: DYN_T_E4M3}
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _packer(cls):
+    """Packs a structure's fields, in their order, to bytes with the C compiler's alignment (NULL is 0): a third of the time of making a ctypes
+    structure, which counts where a step's launches follow each other within microseconds."""
+    codes = {_i32: "i", _i64: "q", _f64: "d", C.c_float: "f", _vp: "P"}
+
+    def code(c):
+        return "".join(code(t) if t not in codes else codes[t] for _, t in c._fields_)
+    p = struct.Struct("@" + code(cls) + "0P")
+    assert p.size == C.sizeof(cls)
+    return p.pack
+
+
+_pack_requests, _pack_plan, _pack_append, _pack_attention = (_packer(c) for c in (_KvRequests, _KvPlan, _Append, _Attention))
 
 
 def _type(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in _TYPES:
+    k = _TYPES.get(t.dtype)
+    if k is None:
         raise ValueError(f"{name} must be float16, bfloat16 or (a cache) float8_e4m3fn, got {t.dtype}")
-    return _TYPES[t.dtype]
+    return k
 
 
-def _rows(t: torch.Tensor, name: str, shape, dtype) -> _Rows:
-    """[n_token][heads][head_dim] with neighbouring elements of a head side by side; any other strides."""
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape or t.stride(2) != 1:
-        raise ValueError(f"{name} must be a GPU tensor of {dtype} and shape {tuple(shape)} whose last dimension is contiguous")
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _at(t: torch.Tensor, dtype, name: str) -> int:
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous GPU tensor of {dtype}")
+    return t.data_ptr()
 
 
-def _scale(t: Optional[torch.Tensor], n: int, name: str):
-    if t is not None and t.numel() != n:
+def _rows(t: torch.Tensor, name: str, shape, dtype):
+    """Address and strides of [n_token][heads][head_dim] with neighbouring elements of a head side by side; any other strides."""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor of {dtype} and shape {tuple(shape)}")
+    token, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), token, head
+
+
+def _scale(t: Optional[torch.Tensor], n: int, name: str) -> int:
+    if t is None:
+        return 0
+    if t.numel() != n:
         raise ValueError(f"{name} must have one factor per key head")
-    return _dp(t, torch.float32, name)
+    return _at(t, _F32, name)
 
 
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor):
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
         raise ValueError("k_cache and v_cache must be alike, [n_page][n_kv_head][page_tokens][head_dim]")
-    return _dp(k_cache, None, "k_cache"), _dp(v_cache, None, "v_cache"), _type(k_cache, "k_cache")
+    dtype = k_cache.dtype
+    return _at(k_cache, dtype, "k_cache"), _at(v_cache, dtype, "v_cache"), _type(k_cache, "k_cache")
+
+
+def _raw_stream(stream) -> int:          # the tensors are on the GPU by now: nothing is left to initialise
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
+def _fill(t: torch.Tensor, name: str):
+    """Address and bytes of a workspace."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous GPU tensor")
+    return t.data_ptr(), t.nbytes
 
 
 def dyn_kv_step_workspace(n_req: int) -> int:
     return int(_lib.dyn_kv_step_workspace(n_req))
 
 
+class KvStep(dict):
+    """What a step's tokens and requests get, by name; `workspace` is the one that the call used (its status: dyn_workspace_status)."""
+    __slots__ = ("workspace",)
+
+
 def dyn_kv_step(ctx_len: torch.Tensor, new_len: torch.Tensor, n_token: int, block_table: torch.Tensor, free_pages: torch.Tensor,
-                free_state: torch.Tensor, page_tokens: int, workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+                free_state: torch.Tensor, page_tokens: int, workspace: Optional[torch.Tensor] = None, stream=None) -> KvStep:
     """Block tables and slot maps of a step.  block_table and free_pages are updated in place; returns cu_new, kv_len, next_len, pos,
-    slot, free_state (and the two updated tensors) and the workspace, whose status dyn_workspace_status reads."""
-    B, dev = ctx_len.numel(), ctx_len.device
-    if new_len.numel() != B or block_table.dim() != 2 or block_table.shape[0] != B or free_state.numel() != 2:
+    slot, free_state and the two updated tensors."""
+    B = ctx_len.numel()
+    if block_table.dim() != 2 or new_len.numel() != B or block_table.shape[0] != B or free_state.numel() != 2:
         raise ValueError("ctx_len, new_len [n_req], block_table [n_req][max_pages] and free_state [2] do not fit together")
-    i32 = torch.int32
-    r = _KvRequests(B, n_token, page_tokens, free_pages.numel(), block_table.shape[1], _dp(ctx_len, i32, "ctx_len"), _dp(new_len, i32, "new_len"),
-                    _dp(block_table, i32, "block_table"), _dp(free_pages, i32, "free_pages"), _dp(free_state, i32, "free_state"))
+    if n_token < 0:
+        raise ValueError("n_token < 0")
+    r = _pack_requests(B, n_token, page_tokens, free_pages.numel(), block_table.shape[1], _at(ctx_len, _I32, "ctx_len"), _at(new_len, _I32, "new_len"),
+                       _at(block_table, _I32, "block_table"), _at(free_pages, _I32, "free_pages"), _at(free_state, _I32, "free_state"))
     # one allocation for what is returned and the workspace, which comes first
-    own = 0 if workspace is not None else (dyn_kv_step_workspace(B) + 3) // 4
-    base = torch.empty(own + 3 * B + 3 + 2 * n_token, dtype=i32, device=dev)
-    parts = base.split_with_sizes([own, B + 1, B, B, n_token, n_token, 2])
-    p = base.data_ptr() + 4 * own
-    plan = _KvPlan(p, p + 4 * (B + 1), p + 4 * (2 * B + 1), p + 4 * (3 * B + 1), p + 4 * (3 * B + 1 + n_token), p + 4 * (3 * B + 1 + 2 * n_token))
-    if workspace is None:
-        workspace, ws, nbytes = parts[0], base.data_ptr(), 4 * own
-    else:
-        ws, nbytes = _dp(workspace), workspace.numel() * workspace.element_size()
-    _check(_lib.dyn_kv_step(C.byref(r), C.byref(plan), ws, nbytes, _stream(stream)), "dyn_kv_step")
-    return {"cu_new": parts[1], "kv_len": parts[2], "next_len": parts[3], "pos": parts[4], "slot": parts[5], "block_table": block_table,
-            "free_pages": free_pages, "free_state": parts[6], "workspace": workspace}
+    own = 0 if workspace is not None else _lib.dyn_kv_step_workspace(B) >> 2        # a multiple of 256 bytes
+    base = torch.empty(own + 3 * B + 3 + 2 * n_token, dtype=_I32, device=ctx_len.device)
+    mine, cu, kv, nxt, pos, slot, state = base.split_with_sizes([own, B + 1, B, B, n_token, n_token, 2])
+    ws, nbytes = base.data_ptr(), 4 * own
+    p = ws + nbytes
+    plan = _pack_plan(p, p + 4 * (B + 1), p + 4 * (2 * B + 1), p + 4 * (3 * B + 1), p + 4 * (3 * B + 1 + n_token), p + 4 * (3 * B + 1 + 2 * n_token))
+    if workspace is not None:
+        mine, (ws, nbytes) = workspace, _fill(workspace, "workspace")
+    _check(_lib.dyn_kv_step(r, plan, ws, nbytes, _raw_stream(stream)), "dyn_kv_step")
+    out = KvStep(cu_new=cu, kv_len=kv, next_len=nxt, pos=pos, slot=slot, block_table=block_table, free_pages=free_pages, free_state=state)
+    out.workspace = mine
+    return out
 
 
 def dyn_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = DYN_ROPE_PLAIN, factor: float = 1.0, original_tokens: float = 0.0,
@@ -815,19 +862,19 @@ def dyn_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torc
     q [n_token][n_q_head][head_dim], k and v [n_token][n_kv_head][head_dim] (views of one product's output will do)."""
     if q.dim() != 3:
         raise ValueError("q must be [n_token][n_q_head][head_dim]")
-    T, H, D = q.shape
+    shape, dtype = q.shape, q.dtype
+    T, H, D = shape
     kc, vc, ct = _cache(k_cache, v_cache)
     N, G, P, Dc = k_cache.shape
     if Dc != D or pos.numel() != T or slot.numel() != T:
         raise ValueError("queries, cache, pos and slot do not fit together")
     w = _host(inv_freq, np.float64)
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
-    a = _Append(T, H, G, D, _type(q, "q"), ct, P, N, _rows(q, "q", q.shape, q.dtype), _rows(k, "k", (T, G, D), q.dtype),
-                _rows(v, "v", (T, G, D), q.dtype), _rows(out, "out", (T, H, D), q.dtype), _dp(pos, torch.int32, "pos"),
-                _dp(slot, torch.int32, "slot"), kc, vc, _scale(k_scale, G, "k_scale"), _scale(v_scale, G, "v_scale"), 2 * w.size,
-                int(interleaved), _hp(w), rope_scale)
-    _check(_lib.dyn_rope_append(C.byref(a), _stream(stream)), "dyn_rope_append")
+        out = torch.empty((T, H, D), dtype=dtype, device=q.device)
+    a = _pack_append(T, H, G, D, _type(q, "q"), ct, P, N, *_rows(q, "q", shape, dtype), *_rows(k, "k", (T, G, D), dtype), *_rows(v, "v", (T, G, D), dtype),
+                     *_rows(out, "out", shape, dtype), _at(pos, _I32, "pos"), _at(slot, _I32, "slot"), kc, vc, _scale(k_scale, G, "k_scale"),
+                     _scale(v_scale, G, "v_scale"), 2 * w.size, int(interleaved), w.__array_interface__["data"][0], rope_scale)
+    _check(_lib.dyn_rope_append(a, _raw_stream(stream)), "dyn_rope_append")
     return out
 
 
@@ -845,20 +892,20 @@ def dyn_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     saves an allocation and a fill per call, and can read its status."""
     if q.dim() != 3 or block_table.dim() != 2:
         raise ValueError("q must be [n_token][n_q_head][head_dim], block_table [n_req][max_pages]")
-    T, H, D = q.shape
+    shape, dtype = q.shape, q.dtype
+    T, H, D = shape
     kc, vc, ct = _cache(k_cache, v_cache)
     N, G, P, Dc = k_cache.shape
-    B = block_table.shape[0]
+    B, cols = block_table.shape
     if Dc != D or cu_new.numel() != B + 1 or kv_len.numel() != B:
         raise ValueError("queries, cache, block_table, cu_new and kv_len do not fit together")
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        out = torch.empty((T, H, D), dtype=dtype, device=q.device)
     if workspace is None:
         workspace = torch.empty(max(256, dyn_paged_attention_workspace(B, T, H, G, D, max_new, max_kv)), dtype=torch.uint8, device=q.device)
         workspace[:256].zero_()
-    a = _Attention(B, T, H, G, D, _type(q, "q"), ct, P, N, block_table.shape[1], max_new, max_kv, window, n_sink,
-                   D ** -0.5 if scale is None else scale, _rows(q, "q", q.shape, q.dtype), _rows(out, "out", (T, H, D), q.dtype), kc, vc,
-                   _scale(k_scale, G, "k_scale"), _scale(v_scale, G, "v_scale"), _dp(block_table, torch.int32, "block_table"),
-                   _dp(cu_new, torch.int32, "cu_new"), _dp(kv_len, torch.int32, "kv_len"))
-    _check(_lib.dyn_paged_attention(C.byref(a), _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "dyn_paged_attention")
+    a = _pack_attention(B, T, H, G, D, _type(q, "q"), ct, P, N, cols, max_new, max_kv, window, n_sink, D ** -0.5 if scale is None else scale,
+                        *_rows(q, "q", shape, dtype), *_rows(out, "out", shape, dtype), kc, vc, _scale(k_scale, G, "k_scale"),
+                        _scale(v_scale, G, "v_scale"), _at(block_table, _I32, "block_table"), _at(cu_new, _I32, "cu_new"), _at(kv_len, _I32, "kv_len"))
+    _check(_lib.dyn_paged_attention(a, *_fill(workspace, "workspace"), _raw_stream(stream)), "dyn_paged_attention")
     return out

@@ -1,4 +1,4 @@
-// Device-side parts shared by the two attention kernels and the kernel that joins their pieces.
+// Device-side parts shared by the two attention kernels and the kernels that join their pieces.
 //
 // Row (token i of request b, query head h) stands at p = kv_len - n + i and sees the keys j <= p with j > p - window or j < n_sink:
 //   o = sum_j exp(c q.k_j - m) v_j / sum_j exp(c q.k_j - m),   c = scale x the key head's scale,
@@ -81,8 +81,6 @@ __device__ __forceinline__ Keys keys_of(const AttnArgs& a, int32_t lo, int32_t h
   }
   return k;
 }
-// The pieces that the tiles are cut into: the last one has what is left.
-__device__ __forceinline__ int pieces_of(const Keys& k, int32_t n_chunk, int32_t each) { return max(1, min(n_chunk, (k.count + each - 1) / each)); }
 __device__ __forceinline__ int32_t tile_of(const Keys& k, int32_t v) { return v < k.sink_tiles ? v : v - k.sink_tiles + k.first; }
 
 // Whether some row from position `first` to `last` does not see every key of a tile.
@@ -124,22 +122,28 @@ __device__ __forceinline__ float factor_of(const AttnArgs& a, int kvh) {
 }
 __device__ __forceinline__ float size_of(float factor) { return fmaxf(fabsf(factor), 1e-30f); }
 
-// 8 elements of a query row.
-template <typename T>
-__device__ __forceinline__ x8<T> load_query(const AttnArgs& a, const T* src, bool in, uint32_t flip) {
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (in) {
-    if (a.q_vec) {
-      v = *(const u32x4*)src;
-    } else {
-      const uint16_t* p = (const uint16_t*)src;
+// N times 8 elements of a query row, the i-th from element at(i): zeros beyond the head's end and where there is no row (`src` is a row all the same).  All loads are in
+// flight together: a branch around each would have them wait for one another.
+template <typename T, int N, typename At>
+__device__ __forceinline__ void load_query(const AttnArgs& a, const T* src, bool in, uint32_t flip, At at, x8<T>* q) {
+  u32x4 v[N];
+  if (a.q_vec) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = p[2 * j] | (uint32_t)p[2 * j + 1] << 16;
+    for (int i = 0; i < N; ++i) v[i] = *(const u32x4*)(src + (at(i) < a.head_dim ? at(i) : 0));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint16_t* p = (const uint16_t*)src + (at(i) < a.head_dim ? at(i) : 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = p[2 * j] | (uint32_t)p[2 * j + 1] << 16;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] ^= flip;
   }
-  return __builtin_bit_cast(x8<T>, v);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i][j] = in && at(i) < a.head_dim ? v[i][j] ^ flip : 0u;
+    q[i] = __builtin_bit_cast(x8<T>, v[i]);
+  }
 }
 
 // 4 neighbouring elements of an output row.
@@ -154,11 +158,6 @@ __device__ __forceinline__ void store4(T* p, const float* x, bool vec) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = (T)x[i];
   }
-}
-
-// Where a row's pieces lie: token and head.
-__device__ __forceinline__ int64_t part_row(const AttnArgs& a, int chunk, int64_t t, int head) {
-  return ((int64_t)chunk * a.n_token + t) * (a.n_kv_head * a.group) + head;
 }
 
 // The page of a key; an entry outside the cache is read as one inside and reported (`bad`).
@@ -185,6 +184,16 @@ __device__ __forceinline__ bool by_sixteen(const AttnArgs& a, int32_t key0, int 
 __device__ __forceinline__ int64_t row_at(const AttnArgs& a, int kvh, int32_t key, int32_t page) {
   return (int64_t)((uint64_t)(uint32_t)page * a.page_bytes) + (((uint32_t)kvh << a.page_shift) + (uint32_t)(key & ((1 << a.page_shift) - 1))) * a.row_bytes;
 }
+
+// Bits 15 and 31 of the union of these say whether one of 8 values is not finite.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(u32x4 x) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= (x[i] & 0x7fff7fffu) + Kind<T>::carry;
+  return odd;
+}
+__device__ __forceinline__ bool any_not_finite(uint32_t odd) { return __any((odd & 0x80008000u) != 0); }
 
 // 8 values on their way to LDS.  Those that are not finite are taken out and marked, a bit for +inf (`up`) and one for -inf (`down`), both for what is not a
 // number.

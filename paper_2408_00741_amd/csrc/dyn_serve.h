@@ -43,15 +43,17 @@ struct AttnArgs {
   int32_t blocks_narrow;          // blocks of the narrow kernel, equal parts of all keys; 0: one for each request and key head
   int4* cuts;                     // workspace [blocks_narrow]: the pair that goes on beyond a block's part (request, key head, last block, slot), request -1: none
   float* piece; float* piece_ml;  // workspace: [blocks_narrow][2][rows_narrow][head_dim] and [..][2]
-  // wide kernel: the key axis is cut in at most n_chunk_wide pieces of `tiles_wide` tiles
-  int32_t n_chunk_wide, tiles_wide;
   int32_t n_tile_wide;            // row tiles of the wide kernel at most, 0: none
-  float* part; float* part_ml;    // workspace: [chunk][token][head][head_dim] and [chunk][token][head][2]
+  int32_t blocks_wide;            // blocks of the wide kernel, which deal out the pairs of a row tile and a key head; 0: one for each pair
+  int4* cuts_wide;                // workspace [blocks_wide]: the pair that goes on beyond a block's part (row tile, key head, last block, slot), row tile -1: none
+  float* part; float* part_ml;    // workspace: [blocks_wide][2][rows of a tile][head_dim] and [..][2]
   WsHeader* header;
 };
 hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s);
 #define DYN_ATTN_KEYS_NARROW 32   // keys of a tile
 #define DYN_ATTN_KEYS_WIDE 64
-#define DYN_ATTN_WAVES_WIDE 4     // waves of a block of the wide kernel, each with rows of its own
+#define DYN_ATTN_WAVES_WIDE 4     // waves of a block of the wide kernel, each with 32 rows of its own
+#define DYN_ATTN_BLOCKS 512       // two for each compute unit, in either kernel: what is resident at a time
+#define DYN_ATTN_PAIRS_WIDE 2048  // row tiles x key heads up to which the wide kernel's blocks deal them out
 
 #endif  // DYN_SERVE_H_

@@ -127,12 +127,10 @@ namespace {
 
 // How the launches are shaped, and the places in the workspace.
 struct AttnShape {
-  int32_t rows_narrow, rows_most, blocks_narrow, n_chunk_wide, tiles_wide, n_tile_wide;
-  size_t piece_ml, piece, ml, part, total;
+  int32_t rows_narrow, rows_most, blocks_narrow, n_tile_wide, blocks_wide;
+  size_t piece_ml, piece, cuts_wide, part_ml, part, total;
 };
-constexpr int32_t kBlocksNarrow = 512;       // two for each compute unit: what is resident at a time
 constexpr int64_t kPairs = 4096;             // requests x key heads from which a block is a pair: the card's own order evens them out, and every block's sum over all requests would cost more
-constexpr size_t kPartBytes = 64u << 20;     // sums of the wide kernel's pieces at most
 
 AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int32_t n_kv_head, int32_t head_dim, int32_t max_new, int32_t max_kv, int32_t window,
                           int32_t n_sink) {
@@ -140,32 +138,28 @@ AttnShape attention_shape(int32_t n_req, int32_t n_token, int32_t n_q_head, int3
   const int64_t group = n_q_head / n_kv_head, rows = (int64_t)std::min(max_new, n_token) * group;
   const int64_t seen = window > 0 ? std::min<int64_t>(max_kv, (int64_t)window + max_new + n_sink + 2 * DYN_ATTN_KEYS_WIDE) : max_kv;
   // Steps of up to 32 rows a request take the narrow kernel alone, with 16 rows in half the registers where that is enough; where some request has more, those
-  // of 17 to 32 go with them.
-  s.rows_narrow = rows > 16 && rows <= 32 ? 32 : 16;
+  // of up to 16 go with it.  Where none can have so few (given that every token is a request's), the wide kernel takes whatever there is: two launches that find nothing to do
+  // cost 10 us.
+  const int64_t fewest = (n_token - (int64_t)(n_req - 1) * max_new) * group;
+  s.rows_narrow = rows <= 16 ? 16 : rows <= 32 ? 32 : fewest > 32 ? 0 : 16;
   s.rows_most = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rows, s.rows_narrow));
   // a block for each unit (four tiles of keys) where they are few
-  const int64_t pairs = (int64_t)n_req * n_kv_head, units = pairs * ((seen + 4 * DYN_ATTN_KEYS_NARROW - 1) / (4 * DYN_ATTN_KEYS_NARROW) + 1);
-  s.blocks_narrow = pairs < kPairs ? (int32_t)std::min<int64_t>(kBlocksNarrow, units) : 0;
-  s.n_tile_wide = 0;
-  s.n_chunk_wide = s.tiles_wide = 1;
-  int64_t chunks = 1;
+  const int64_t pairs = s.rows_narrow ? (int64_t)n_req * n_kv_head : 0, units = pairs * ((seen + 4 * DYN_ATTN_KEYS_NARROW - 1) / (4 * DYN_ATTN_KEYS_NARROW) + 1);
+  s.blocks_narrow = pairs < kPairs ? (int32_t)std::min<int64_t>(DYN_ATTN_BLOCKS, units) : 0;
+  s.n_tile_wide = s.blocks_wide = 0;
+  constexpr int64_t R = 32 * DYN_ATTN_WAVES_WIDE;
   if (rows > 32) {
-    const int64_t R = 32 * DYN_ATTN_WAVES_WIDE, all = (int64_t)n_token * group, tiles = (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE;
-    s.n_tile_wide = (int32_t)(all / R + n_req);
-    const int64_t blocks = std::max<int64_t>(1, all / R) * n_kv_head;
-    // few row tiles: the keys are cut until there are two blocks for each compute unit, pieces of at least 4 tiles; the workspace holds as many pieces as were
-    // wanted: never fewer for more keys
-    chunks = std::min<int64_t>((512 + blocks - 1) / blocks, std::max<int64_t>(1, tiles / 4));
-    chunks = std::min<int64_t>(chunks, std::max<int64_t>(1, (int64_t)kPartBytes / std::max<int64_t>((int64_t)n_token * n_q_head * (head_dim + 2) * 4, 1)));
-    s.tiles_wide = (int32_t)std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
-    s.n_chunk_wide = (int32_t)std::max<int64_t>(1, (tiles + s.tiles_wide - 1) / s.tiles_wide);
+    const int64_t tiles = (int64_t)n_token * group / R + n_req, each = (seen + DYN_ATTN_KEYS_WIDE - 1) / DYN_ATTN_KEYS_WIDE + 1;
+    s.n_tile_wide = (int32_t)tiles;
+    if (tiles * n_kv_head <= DYN_ATTN_PAIRS_WIDE) s.blocks_wide = (int32_t)std::min<int64_t>(DYN_ATTN_BLOCKS, tiles * n_kv_head * each);
   }
-  const size_t pieces = (size_t)s.blocks_narrow * 2 * s.rows_narrow;
+  const size_t pieces = (size_t)s.blocks_narrow * 2 * s.rows_narrow, parts = (size_t)s.blocks_wide * 2 * R;
   s.piece_ml = 256 + align256((size_t)s.blocks_narrow * sizeof(int4));
   s.piece = s.piece_ml + align256(pieces * 2 * sizeof(float));
-  s.ml = s.piece + align256(pieces * head_dim * sizeof(float));
-  s.part = s.ml + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * 2 * sizeof(float)) : 0);
-  s.total = s.part + (chunks > 1 ? align256((size_t)chunks * n_token * n_q_head * head_dim * sizeof(float)) : 0);
+  s.cuts_wide = s.piece + align256(pieces * head_dim * sizeof(float));
+  s.part_ml = s.cuts_wide + align256((size_t)s.blocks_wide * sizeof(int4));
+  s.part = s.part_ml + align256(parts * 2 * sizeof(float));
+  s.total = s.part + align256(parts * head_dim * sizeof(float));
   return s;
 }
 
@@ -207,11 +201,11 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.row_bytes = (uint32_t)row_bytes; a.page_bytes = (uint32_t)page_bytes;
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
   a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow; a.rows_most = s.rows_most;
-  a.blocks_narrow = s.blocks_narrow; a.n_chunk_wide = s.n_chunk_wide; a.tiles_wide = s.tiles_wide; a.n_tile_wide = s.n_tile_wide;
+  a.blocks_narrow = s.blocks_narrow; a.n_tile_wide = s.n_tile_wide; a.blocks_wide = s.blocks_wide;
   char* base = (char*)workspace;
   a.header = (WsHeader*)base;
   a.cuts = (int4*)(base + 256); a.piece_ml = (float*)(base + s.piece_ml); a.piece = (float*)(base + s.piece);
-  a.part_ml = (float*)(base + s.ml); a.part = (float*)(base + s.part);
+  a.cuts_wide = (int4*)(base + s.cuts_wide); a.part_ml = (float*)(base + s.part_ml); a.part = (float*)(base + s.part);
   return hip_ok(dyn_launch_paged_attention(a, (hipStream_t)hip_stream), "attention launch") ? DYN_OK : DYN_E_DEVICE;
 }
 

@@ -74,8 +74,15 @@ template <typename T, bool F8, int DP>
 struct Values {
   static constexpr int kPerRow = F8 ? DP / 16 : DP / 8, kRows = 64 / kPerRow, kEach = KT / kRows;
   u32x4 x[kEach];
-  __device__ __forceinline__ void write(u32x4* lds, bool mark, uint8_t* marks) {
+  // Returns whether values that are not finite were taken out; `mark`: they have to be.
+  __device__ __forceinline__ bool write(u32x4* lds, bool mark, uint8_t* marks) {
     const int lane = threadIdx.x & 63, c = lane % kPerRow;
+    if (mark) {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) odd |= F8 ? not_finite<T>(widen(T{}, x[i][0], x[i][1])) | not_finite<T>(widen(T{}, x[i][2], x[i][3])) : not_finite<T>(x[i]);
+      mark = any_not_finite(odd);
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int row = lane / kPerRow + i * kRows;
@@ -87,14 +94,15 @@ struct Values {
         lds[v_at<DP>(row, c8)] = v;
       }
     }
+    return mark;
   }
 };
 
 // From the scores of a tile to the weighted sum of its values in LDS.
 template <typename T, int DP, int NT>
-__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32x4 (*s)[2], const u32x4* lds, bool marked, const uint32_t* marks, int32_t key0) {
+__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32x4 (*s)[2], const u32x4* lds, bool hidden, bool marked, const uint32_t* marks, int32_t key0) {
   const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
-  if (marked) {      // some row does not see every key: what it does not see scores -inf, weight 0 below, whatever the reference
+  if (hidden) {      // some row does not see every key: what it does not see scores -inf, weight 0 below, whatever the reference
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int32_t mine = key0 + 8 * anew(g), from = a.window > 0 ? r.low[n] - mine : -1, upto = r.pos[n] - mine;      // seen: from < key <= upto, and the first tokens
@@ -146,21 +154,17 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32
   }
   // values that are not finite were taken out and marked: they go to the rows that see their keys
   if (marked) {
-    uint32_t any = 0;
-    for (int i = lane; i < 2 * KT * DP / 32; i += 64) any |= marks[i];
-    if (__any(any != 0)) {
-      for (int key = 0; key < KT; ++key) {
-        const int32_t at = key0 + key;
+    for (int key = 0; key < KT; ++key) {
+      const int32_t at = key0 + key;
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-          const int word = t / 2, shift = 16 * (t % 2) + 4 * g;
-          const uint32_t up = marks[key * (DP / 32) + word] >> shift, down = marks[(KT + key) * (DP / 32) + word] >> shift;
+      for (int t = 0; t < DP / 16; ++t) {
+        const int word = t / 2, shift = 16 * (t % 2) + 4 * g;
+        const uint32_t up = marks[key * (DP / 32) + word] >> shift, down = marks[(KT + key) * (DP / 32) + word] >> shift;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = marked_value(up, down, i);
+        for (int i = 0; i < 4; ++i) {
+          const float x = marked_value(up, down, i);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) r.o[n][t][i] += at <= r.pos[n] && (at > r.low[n] || at < a.n_sink) ? x : 0.0f;
-          }
+          for (int n = 0; n < NT; ++n) r.o[n][t][i] += at <= r.pos[n] && (at > r.low[n] || at < a.n_sink) ? x : 0.0f;
         }
       }
     }
@@ -282,11 +286,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
     for (int n = 0; n < NT; ++n) {
       const int32_t row = 16 * n + n16, i = min(row, rows - 1) / a.group, h = min(row, rows - 1) - i * a.group;
       const T* src = (const T*)a.q + (int64_t)(q.t0 + i) * a.q_token + (int64_t)(kvh * a.group + h) * a.q_head;
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
-        const int at = KeyRows<T, F8, DP>::element(d, g);
-        r.q[n][d] = load_query<T>(a, src + at, row < rows && at < a.head_dim, factor < 0.0f ? 0x80008000u : 0u);
-      }
+      load_query<T, DP / 32>(a, src, row < rows, factor < 0.0f ? 0x80008000u : 0u, [&](int d) { return KeyRows<T, F8, DP>::element(d, g); }, r.q[n]);
       r.pos[n] = row < rows ? q.len - q.n + i : -1;
       r.low[n] = a.window > 0 ? r.pos[n] - a.window : -1;
       r.m[n] = -INFINITY;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
       load_values(v, next);
       for (; v < v1; v += 4) {
         const int32_t key0 = tile_of(keys, v) * KT;
-        const bool marked = hides<KT>(a, r.first, r.last, key0);
+        const bool hidden = hides<KT>(a, r.first, r.last, key0);
         f32x4 s[NT][2];
         kr.scores(row_bytes, r, s);
         __builtin_amdgcn_sched_barrier(0);     // what is loaded next takes the registers that are free now, not others
@@ -361,14 +361,14 @@ __global__ __launch_bounds__(256, 2) void attend_narrow_kernel(AttnArgs a) {
           fetch(v + 8);
           load_keys(v + 4, next);
         }
-        values.write(lds, marked, (uint8_t*)s_marks[wave]);
+        const bool marked = values.write(lds, hidden, (uint8_t*)s_marks[wave]);
         if (v + 4 < v1) {
           load_values(v + 4, next);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        weigh<T, DP, NT>(a, r, s, lds, marked, s_marks[wave], key0);
+        weigh<T, DP, NT>(a, r, s, lds, hidden, marked, s_marks[wave], key0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }

@@ -369,7 +369,7 @@ def _check_step(ctx, new, table, ring, state, page):
     want = plain.step(ctx, new, table, ring, state, page, T)
     for name, w in zip(("cu_new", "kv_len", "next_len", "pos", "slot", "block_table", "free_pages", "free_state"), want):
         assert np.array_equal(p[name].cpu().numpy(), w), name
-    assert dyn.dyn_workspace_status(p["workspace"]) == (dyn.DYN_WS_NO_PAGES if any(want[-1]) else 0)
+    assert dyn.dyn_workspace_status(p.workspace) == (dyn.DYN_WS_NO_PAGES if any(want[-1]) else 0)
     return p
 
 
@@ -416,14 +416,14 @@ def test_step_with_lengths_that_cannot_be():
             a[4], n[4] = cx, nw
             tab = np.resize(table, (B, table.shape[1])).astype(np.int32)
             p = dyn.dyn_kv_step(c(a), c(n), t, c(tab), c(ring), c(state), 16)
-            assert dyn.dyn_workspace_status(p["workspace"]) & dyn.DYN_WS_BAD_REQUEST, (B, k)
+            assert dyn.dyn_workspace_status(p.workspace) & dyn.DYN_WS_BAD_REQUEST, (B, k)
             slot = p["slot"].cpu().numpy()
             assert slot.min() >= -1 and slot.max() < ring.size * 16
             cu = p["cu_new"].cpu().numpy()
             assert np.all(np.diff(cu) >= 0) and cu[-1] <= t
     bad = np.array([-3, 10 ** 6], np.int32)
     p = dyn.dyn_kv_step(c(ctx), c(new), T, c(table), c(ring), c(bad), 16)
-    assert dyn.dyn_workspace_status(p["workspace"]) & dyn.DYN_WS_BAD_PAGE
+    assert dyn.dyn_workspace_status(p.workspace) & dyn.DYN_WS_BAD_PAGE
 
 
 # ---- the three together --------------------------------------------------------------------------------------------
