@@ -243,6 +243,6 @@ __device__ __forceinline__ u32x4 read_values(const __attribute__((address_space(
 }  // namespace
 
 hipError_t dyn_launch_attend_narrow(const AttnArgs& a, hipStream_t s);
-hipError_t dyn_launch_attend_wide(const AttnArgs& a, hipStream_t s);
+hipError_t dyn_launch_attend_mixed(const AttnArgs& a, hipStream_t s);
 
 #endif  // DYN_ATTN_H_

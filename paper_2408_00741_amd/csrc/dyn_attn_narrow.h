@@ -1,0 +1,511 @@
+// Attention for requests of few rows (new tokens x query heads of a key head): one new token each, or a few.
+#ifndef DYN_ATTN_NARROW_H_
+#define DYN_ATTN_NARROW_H_
+
+#include "dyn_attn.h"
+
+namespace {
+namespace narrow {
+
+__device__ __forceinline__ f32x4 mfma(x8<__bf16> a, x8<__bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma(x8<_Float16> a, x8<_Float16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+constexpr int KT = DYN_ATTN_KEYS_NARROW;   // 32 keys: two of the first product's left operands, one of the second product's steps
+
+// Row n (lane % 16) of left operand t is key 8 (n / 4) + 4 t + n % 4 of the tile: lane group g = lane / 16 then has the scores of keys 8 g + 4 t + i, the 8
+// neighbouring keys that the second product wants of it.
+__device__ __forceinline__ int key_of_row(int t, int n) { return 8 * (n >> 2) + 4 * t + (n & 3); }
+
+// Where 8 elements of a value row lie in LDS, in units of 16 bytes: turned by the key so that the 4 keys x 32 bytes that two lane groups (keys 8 apart) read at
+// a time hit all 64 banks.
+template <int DP>
+constexpr int kRow = DP / 8;
+template <int DP>
+__device__ __forceinline__ int v_at(int key, int c8) {
+  return DP == 128 ? key * 16 + (c8 ^ ((key & 3) << 2) ^ ((key >> 3 & 1) << 1)) : key * 8 + (c8 ^ ((key >> 1 & 1) << 2) ^ ((key >> 3 & 1) << 1));
+}
+
+template <typename T, int DP, int NT>
+struct Rows {
+  x8<T> q[NT][DP / 32];      // right operand of the first product: row lane % 16
+  f32x4 o[NT][DP / 16];      // O^T: element 16 t + 4 (lane / 16) + i
+  float m[NT], sum[NT], c;   // reference (before c), sum of this lane's weights, the scores' factor
+  int32_t pos[NT], low[NT];  // position (-1: no row), last key that the window hides
+  int32_t first, last;       // least and greatest position
+};
+
+// Two left operands straight from the cache, 16 bytes a load.  In 8 bits a load is two steps of the product: step d takes the elements
+// 64 (d / 2) + 16 g + 8 (d % 2) .. of a head, in the queries too.
+template <typename T, bool F8, int DP>
+struct KeyRows {
+  static constexpr int kLoads = F8 ? DP / 64 : DP / 32;
+  u32x4 x[2][kLoads];
+  static __device__ __forceinline__ int element(int d, int g) { return F8 ? 64 * (d / 2) + 16 * g + 8 * (d % 2) : 32 * d + 8 * g; }
+  __device__ __forceinline__ void load(const char* const* at, int row_bytes) {   // at[t]: this lane's row of operand t
+    const int c = 16 * ((threadIdx.x >> 4) & 3);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) x[t][i] = *(const u32x4*)(at[t] + (64 * i + c < row_bytes ? 64 * i + c : 0));
+  }
+  template <int NT>
+  __device__ __forceinline__ void scores(int row_bytes, const Rows<T, DP, NT>& r, f32x4 (*s)[2]) {
+    if (row_bytes < 64 * kLoads) {          // beyond the head's end: zeros, as in the queries
+      const int c = 16 * ((threadIdx.x >> 4) & 3);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) x[t][i] = 64 * i + c < row_bytes ? x[t][i] : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        u32x4 k;
+        if constexpr (F8) k = d % 2 ? widen(T{}, x[t][d / 2][2], x[t][d / 2][3]) : widen(T{}, x[t][d / 2][0], x[t][d / 2][1]);
+        else k = x[t][d];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][t] = mfma(__builtin_bit_cast(x8<T>, k), r.q[n][d], s[n][t]);
+      }
+    }
+  }
+};
+
+// A tile of values on its way to LDS, 16 bytes a load, whole rows by neighbouring lanes.
+template <typename T, bool F8, int DP>
+struct Values {
+  static constexpr int kPerRow = F8 ? DP / 16 : DP / 8, kRows = 64 / kPerRow, kEach = KT / kRows;
+  u32x4 x[kEach];
+  // Returns whether values that are not finite were taken out; `mark`: they have to be.
+  __device__ __forceinline__ bool write(u32x4* lds, bool mark, uint8_t* marks) {
+    const int lane = threadIdx.x & 63, c = lane % kPerRow;
+    if (mark) {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) odd |= F8 ? not_finite<T>(widen(T{}, x[i][0], x[i][1])) | not_finite<T>(widen(T{}, x[i][2], x[i][3])) : not_finite<T>(x[i]);
+      mark = any_not_finite(odd);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int row = lane / kPerRow + i * kRows;
+#pragma unroll
+      for (int e = 0; e < (F8 ? 2 : 1); ++e) {
+        const int c8 = F8 ? 2 * c + e : c;
+        u32x4 v = F8 ? widen(T{}, x[i][2 * e], x[i][2 * e + 1]) : x[i];
+        if (mark) v = take_out<T>(v, marks + row * (DP / 8) + c8, marks + (KT + row) * (DP / 8) + c8);
+        lds[v_at<DP>(row, c8)] = v;
+      }
+    }
+    return mark;
+  }
+};
+
+// From the scores of a tile to the weighted sum of its values in LDS.
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP, NT>& r, f32x4 (*s)[2], const u32x4* lds, bool hidden, bool marked, const uint32_t* marks, int32_t key0) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
+  if (hidden) {      // some row does not see every key: what it does not see scores -inf, weight 0 below, whatever the reference
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int32_t mine = key0 + 8 * anew(g), from = a.window > 0 ? r.low[n] - mine : -1, upto = r.pos[n] - mine;      // seen: from < key <= upto, and the first tokens
+      const uint32_t width = (uint32_t)max(upto - from, 0);
+      const int32_t sinks = a.window > 0 ? min(a.n_sink - mine, upto + 1) : -1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[n][i / 4][i % 4] = (uint32_t)(i - 1 - from) < width || i < sinks ? s[n][i / 4][i % 4] : -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  x8<T> p[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float top = s[n][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[n][i / 4][i % 4]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool raise = (top - r.m[n]) * r.c > kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+    if (__any(raise)) {
+      const float m = fmaxf(r.m[n], top);
+      const float f = r.m[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((r.m[n] - m) * r.c);
+      r.m[n] = m;
+      r.sum[n] *= f;
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.o[n][t][i] *= f;
+    }
+    const float base = Kind<T>::bias - (r.m[n] == -INFINITY ? 0.0f : r.m[n] * r.c);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i / 4][i % 4], r.c, base));
+      sum += w;
+      p[n][i] = (T)w;
+    }
+    r.sum[n] += sum;
+  }
+  typedef const __attribute__((address_space(3))) u32x4* LdsRead;
+  // v_at(.., 2 t + ..) is (at ^ 32 t bytes): a wave's tile begins at a multiple of 256 bytes
+  const uint32_t at = anew(16 * v_at<DP>(8 * g + (i16 >> 2), (i16 & 3) >> 1) + 8 * (i16 & 1)) + (uint32_t)(uintptr_t)(LdsRead)lds;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const LdsRead row = (LdsRead)(uintptr_t)(at ^ 32 * t);
+    const u32x4 v = read_values(row, row + 4 * kRow<DP>);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) r.o[n][t] = mfma(__builtin_bit_cast(x8<T>, v), p[n], r.o[n][t]);
+  }
+  // values that are not finite were taken out and marked: they go to the rows that see their keys
+  if (marked) {
+    for (int key = 0; key < KT; ++key) {
+      const int32_t at = key0 + key;
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) {
+        const int word = t / 2, shift = 16 * (t % 2) + 4 * g;
+        const uint32_t up = marks[key * (DP / 32) + word] >> shift, down = marks[(KT + key) * (DP / 32) + word] >> shift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = marked_value(up, down, i);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) r.o[n][t][i] += at <= r.pos[n] && (at > r.low[n] || at < a.n_sink) ? x : 0.0f;
+        }
+      }
+    }
+  }
+}
+
+// The units (four tiles, one for each wave) of a request's keys; 0: the request is none of this kernel's.  At least one, for rows that see nothing.
+__device__ __forceinline__ Keys keys_of_request(const AttnArgs& a, const Request& q) {
+  return q.len > 0 ? keys_of<KT>(a, q.len - q.n, q.len - 1) : Keys{0, 0, 0};
+}
+__device__ __forceinline__ int32_t units_of(const AttnArgs& a, int b) {
+  if (b >= a.n_req) return 0;
+  const Request q = request_of(a, b);
+  if (q.n == 0 || (int64_t)q.n * a.group > a.rows_narrow) return 0;
+  return max(1, (keys_of_request(a, q).count + 3) / 4);
+}
+
+// What a block does: units [at, end) of the flat range of all (request, key head) pairs' units, one pair after the other.
+struct Share {
+  int64_t all, begin, end, at;
+  int32_t blocks;                // that have a part
+  int32_t b, kvh, unit, units;   // the pair at `at`, and which of its units
+};
+// With a.blocks_narrow blocks each takes an equal part, whatever the requests' lengths are: a block's part may begin and end inside a pair, whose pieces
+// join_narrow_kernel joins.  (Pieces of a fixed length left a third of the card idle where lengths differ: 64 requests of 800 to 8192 tokens 217 us, 600 us for 96 of
+// 8192, which are evenly cut.)  With 0, where the pairs are many, a block is a pair.
+__device__ __forceinline__ Share share_of(const AttnArgs& a, int block) {
+  Share s;
+  if (a.blocks_narrow == 0) {
+    s.b = block / a.n_kv_head;
+    s.kvh = block % a.n_kv_head;
+    s.unit = 0;
+    s.units = units_of(a, s.b);
+    s.all = s.end = s.units;
+    s.begin = s.at = 0;
+    s.blocks = 1;
+    return s;
+  }
+  const int lane = threadIdx.x & 63;
+  s.all = 0;
+  int32_t u = 0;           // of the last 64 requests: all there are in most calls
+  for (int b0 = 0; b0 < a.n_req; b0 += 64) s.all += u = units_of(a, b0 + lane);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) s.all += __shfl_xor(s.all, d);
+  s.all = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s.all >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)s.all));   // known to be the same in all lanes
+  s.all *= a.n_kv_head;
+  s.blocks = (int32_t)min((int64_t)a.blocks_narrow, s.all);      // each of them has a unit at least: no pair goes through a block without one
+  s.b = s.kvh = s.unit = s.units = 0;
+  s.begin = s.end = s.at = 0;
+  if (block >= s.blocks) return s;
+  s.begin = s.at = s.all * block / s.blocks;
+  s.end = s.all * (block + 1) / s.blocks;
+  int64_t before = 0;      // units of the requests before
+  for (int b0 = 0; b0 < a.n_req; b0 += 64) {
+    if (a.n_req > 64) u = units_of(a, b0 + lane);
+    int64_t upto = (int64_t)u * a.n_kv_head;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const unsigned long long past = __ballot(before + upto > s.begin);
+    if (past) {
+      const int l = __ffsll(past) - 1;
+      s.b = __builtin_amdgcn_readfirstlane(b0 + l);
+      s.units = __builtin_amdgcn_readlane(u, l);
+      const int64_t in = s.begin - before - (__shfl(upto, l) - (int64_t)s.units * a.n_kv_head);
+      s.kvh = __builtin_amdgcn_readfirstlane((int)(in / s.units));
+      s.unit = __builtin_amdgcn_readfirstlane((int)(in % s.units));
+      return s;
+    }
+    before += __shfl(upto, 63);
+  }
+  s.end = s.begin;
+  return s;
+}
+
+// Where a block's pieces lie: the one at its part's begin, and the one at its end if that is another.
+__device__ __forceinline__ int64_t piece_row(const AttnArgs& a, int block, int slot, int row) { return ((int64_t)block * 2 + slot) * a.rows_narrow + row; }
+
+// Requests of at most 16 NT rows.  Four waves take the tiles of a piece of a pair's keys in turn, each for all rows, and join at the piece's end.  K goes straight
+// into registers as the left operand, V through LDS; the next tile's loads are in flight while one is worked on.  Bound by the bytes of K and V: 96 requests of
+// 8192 tokens (64 heads over 8, 128 wide, 16 bits) are read at 5.7 TB/s, with the arithmetic left out at 5.7.  Two blocks a compute unit: with three registers
+// are short (5.4).
+template <int DP, int NT>
+struct Lds {
+  u32x4 tile[4][KT * kRow<DP>];           // a wave's values, and at the end the sums of 16 rows
+  uint32_t marks[4][2 * KT * DP / 32];
+  float m[4][16 * NT], sum[4][16 * NT];
+};
+template <typename T, bool F8, int DP, int NT>
+__device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP, NT>& s) {     // s: at a multiple of 256 bytes
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
+  if (block == 0 && tid == 0) a.header->kind = DYN_WS_KIND_WORD;
+  Share sh = share_of(a, block);
+  if (a.blocks_narrow && tid == 0) a.cuts[block] = int4{-1, 0, 0, 0};
+  const int row_bytes = a.head_dim * (F8 ? 1 : 2), quads = a.head_dim / 4;
+  using V = Values<T, F8, DP>;
+  KeyRows<T, F8, DP> kr;
+  V values;
+  u32x4* lds = s.tile[wave];
+  bool bad = false;
+  while (sh.at < sh.end) {
+    const int b = sh.b, kvh = sh.kvh;
+    const int32_t take = (int32_t)min((int64_t)(sh.units - sh.unit), sh.end - sh.at);
+    const bool whole = take == sh.units;
+    const int slot = sh.at == sh.begin ? 0 : 1;
+    if (!whole && sh.unit == 0 && tid == 0) {     // the pair goes on in other blocks, the last of which has its last unit
+      const int64_t pair_end = sh.at + sh.units;
+      a.cuts[block] = int4{b, kvh, (int)((pair_end * sh.blocks + sh.all - 1) / sh.all) - 1, slot};
+    }
+    const Request q = request_of(a, b);
+    const int32_t rows = q.n * a.group;
+    const Keys keys = keys_of_request(a, q);
+    const int32_t v0 = sh.unit * 4, v1 = min(keys.count, (sh.unit + take) * 4);
+    const float factor = factor_of(a, kvh);
+    Rows<T, DP, NT> r;
+    r.c = size_of(factor);
+    r.first = q.len - q.n;
+    r.last = q.len - 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int32_t row = 16 * n + n16, i = min(row, rows - 1) / a.group, h = min(row, rows - 1) - i * a.group;
+      const T* src = (const T*)a.q + (int64_t)(q.t0 + i) * a.q_token + (int64_t)(kvh * a.group + h) * a.q_head;
+      load_query<T, DP / 32>(a, src, row < rows, factor < 0.0f ? 0x80008000u : 0u, [&](int d) { return KeyRows<T, F8, DP>::element(d, g); }, r.q[n]);
+      r.pos[n] = row < rows ? q.len - q.n + i : -1;
+      r.low[n] = a.window > 0 ? r.pos[n] - a.window : -1;
+      r.m[n] = -INFINITY;
+      r.sum[n] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) r.o[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // where the first and the second 16 keys of a tile begin in the cache, in bytes (the tile's end may lie beyond the request's); the table's entries
+    // are fetched a tile before
+    int32_t entry[2];
+    auto fetch = [&](int32_t v) {
+      const int32_t key0 = tile_of(keys, min(v, v1 - 1)) * KT;
+      entry[0] = entry_of_all(a, b, key0);
+      entry[1] = entry_of_all(a, b, min(key0 + 16, q.len - 1));
+    };
+    auto find = [&](int32_t v, int64_t* at) {
+      const int32_t key0 = tile_of(keys, min(v, v1 - 1)) * KT;
+      at[0] = row_at(a, kvh, key0, inside(a, entry[0], &bad));
+      at[1] = row_at(a, kvh, min(key0 + 16, q.len - 1), inside(a, entry[1], &bad));
+    };
+    auto load_keys = [&](int32_t v, const int64_t* at) {
+      const int32_t key0 = tile_of(keys, v) * KT;
+      const char* row[2];
+      if (by_sixteen(a, key0, KT, q.len)) {
+        const char* from = (const char*)a.k_cache + (n16 < 8 ? at[0] : at[1]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) row[t] = from + (key_of_row(t, n16) & 15) * row_bytes;
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int32_t key = min(key0 + key_of_row(t, anew(n16)), q.len - 1);
+          row[t] = (const char*)a.k_cache + row_at(a, kvh, key, page_of(a, b, key, &bad));
+        }
+      }
+      kr.load(row, row_bytes);
+    };
+    auto load_values = [&](int32_t v, const int64_t* at) {
+      const int32_t key0 = tile_of(keys, v) * KT;
+      if (by_sixteen(a, key0, KT, q.len)) {
+        const int c = lane % V::kPerRow * 16;
+        const uint32_t mine = lane / V::kPerRow * row_bytes + (c < row_bytes ? c : 0);
+#pragma unroll
+        for (int i = 0; i < V::kEach; ++i) {
+          const int first = i * V::kRows;
+          values.x[i] = *(const u32x4*)((const char*)a.v_cache + (first < 16 ? at[0] : at[1]) + (first & 15) * row_bytes + mine);
+        }
+      } else {
+        const int l = anew(lane), c = l % V::kPerRow * 16, off = c < row_bytes ? c : 0;
+#pragma unroll
+        for (int i = 0; i < V::kEach; ++i) {
+          const int32_t key = min(key0 + l / V::kPerRow + i * V::kRows, q.len - 1);
+          values.x[i] = *(const u32x4*)((const char*)a.v_cache + row_at(a, kvh, key, page_of(a, b, key, &bad)) + off);
+        }
+      }
+    };
+    int32_t v = v0 + wave;
+    if (v < v1) {
+      int64_t next[2];
+      fetch(v);
+      find(v, next);
+      fetch(v + 4);
+      load_keys(v, next);
+      load_values(v, next);
+      for (; v < v1; v += 4) {
+        const int32_t key0 = tile_of(keys, v) * KT;
+        const bool hidden = hides<KT>(a, r.first, r.last, key0);
+        f32x4 score[NT][2];
+        kr.scores(row_bytes, r, score);
+        __builtin_amdgcn_sched_barrier(0);     // what is loaded next takes the registers that are free now, not others
+        if (v + 4 < v1) {
+          find(v + 4, next);
+          fetch(v + 8);
+          load_keys(v + 4, next);
+        }
+        const bool marked = values.write(lds, hidden, (uint8_t*)s.marks[wave]);
+        if (v + 4 < v1) {
+          load_values(v + 4, next);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        weigh<T, DP, NT>(a, r, score, lds, hidden, marked, s.marks[wave], key0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+
+    // The four waves' sums, O of each in its own tile's place, 16 rows at a time.
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float sum = r.sum[n] + __shfl_xor(r.sum[n], 16);
+      sum += __shfl_xor(sum, 32);
+      if (g == 0) { s.m[wave][16 * n + n16] = r.m[n]; s.sum[wave][16 * n + n16] = sum; }
+    }
+    const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (16 * n >= rows) break;
+      float* s_o = (float*)s.tile[wave];
+      if (16 * n + n16 < rows) {
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) *(f32x4*)&s_o[n16 * DP + 16 * t + 4 * g] = r.o[n][t];
+      }
+      __syncthreads();
+      for (int u = tid; u < min(rows - 16 * n, 16) * quads; u += 256) {
+        const int in = u / quads, rw = 16 * n + in, d = (u % quads) * 4, i = rw / a.group, head = kvh * a.group + (rw - i * a.group);
+        const int64_t t = q.t0 + i;
+        const float m = fmaxf(fmaxf(s.m[0][rw], s.m[1][rw]), fmaxf(s.m[2][rw], s.m[3][rw]));
+        float total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float mw = s.m[w][rw];
+          if (mw == -INFINITY && s.sum[w][rw] == 0.0f) continue;        // no weight in this wave's tiles
+          const float f = mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mw - m) * r.c);
+          total = __builtin_fmaf(s.sum[w][rw], f, total);
+          const f32x4 o = *(const f32x4*)&((const float*)s.tile[w])[in * DP + d];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(o[j], f, x[j]);
+        }
+        if (whole) {
+          const bool none = q.len - q.n + i < 0;
+          const float by = vs / total;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = none ? 0.0f : x[j] * by;
+          store4<T>((T*)a.out + t * a.o_token + (int64_t)head * a.o_head + d, x, a.o_vec);
+        } else {
+          const int64_t at = piece_row(a, block, slot, rw);
+          *(float4*)(a.piece + at * a.head_dim + d) = float4{x[0], x[1], x[2], x[3]};
+          if (d == 0) *(float2*)(a.piece_ml + 2 * at) = float2{m, total};
+        }
+      }
+      __syncthreads();
+    }
+    // the next pair's first unit, if the part goes on
+    sh.at += take;
+    if (sh.at >= sh.end) break;
+    sh.unit = 0;
+    if (++sh.kvh == a.n_kv_head) {
+      sh.kvh = 0;
+      do ++sh.b;
+      while (sh.b < a.n_req && (sh.units = units_of(a, sh.b)) == 0);
+      if (sh.b >= a.n_req) break;
+    }
+  }
+  report(a, bad);
+}
+
+// Joins the pieces of the pairs that were cut: a block for each row of the pair that goes on beyond attend_narrow_kernel's block x.  The waves take the pieces in turn; the
+// sum goes in a fixed order: the same values on every run.  A kernel of its own: a block that waits for the others' pieces, or the last one to come, needs fences over
+// all L2s, which cost more than the launch.
+template <typename T>
+__device__ __forceinline__ void join(const AttnArgs& a, int block, int row) {
+  __shared__ float s_m[4], s_sum[4];
+  __shared__ float2 s_x[4][64];
+  const int4 cut = a.cuts[block];
+  if (cut.x < 0) return;
+  const int b = cut.x, kvh = cut.y, pieces = cut.z - block + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Request q = request_of(a, b);
+  if (row >= q.n * a.group) return;
+  const float c = size_of(factor_of(a, kvh));
+  const bool in = 2 * lane < a.head_dim;
+  float m = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
+  for (int p0 = wave; p0 < pieces; p0 += 32) {
+    float2 ml[8], v[8];
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = min(p0 + 4 * i, pieces - 1);
+      const int64_t at = piece_row(a, block + p, p == 0 ? cut.w : 0, row);
+      ml[i] = *(const float2*)(a.piece_ml + 2 * at);
+      v[i] = *(const float2*)(a.piece + at * a.head_dim + (in ? 2 * lane : 0));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+    const float f0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * c);
+    sum *= f0;
+    x *= f0;
+    y *= f0;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (p0 + 4 * i >= pieces || (ml[i].x == -INFINITY && ml[i].y == 0.0f)) continue;     // no weight in this piece
+      const float f = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
+      sum = __builtin_fmaf(ml[i].y, f, sum);
+      x = __builtin_fmaf(v[i].x, f, x);
+      y = __builtin_fmaf(v[i].y, f, y);
+    }
+  }
+  if (lane == 0) { s_m[wave] = m; s_sum[wave] = sum; }
+  s_x[wave][lane] = float2{x, y};
+  __syncthreads();
+  if (wave != 0 || !in) return;
+  const float all = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  sum = x = y = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (s_m[w] == -INFINITY && s_sum[w] == 0.0f) continue;
+    const float f = s_m[w] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s_m[w] - all) * c);
+    sum = __builtin_fmaf(s_sum[w], f, sum);
+    x = __builtin_fmaf(s_x[w][lane].x, f, x);
+    y = __builtin_fmaf(s_x[w][lane].y, f, y);
+  }
+  const int32_t i = row / a.group;
+  const int64_t t = q.t0 + i;
+  const bool none = q.len - q.n + i < 0;
+  const float by = (a.v_scale ? a.v_scale[kvh] : 1.0f) / sum;
+  T* to = (T*)a.out + t * a.o_token + (int64_t)(kvh * a.group + row - i * a.group) * a.o_head + 2 * lane;
+  to[0] = (T)(none ? 0.0f : x * by);
+  to[1] = (T)(none ? 0.0f : y * by);
+}
+
+}  // namespace narrow
+}  // namespace
+
+#endif  // DYN_ATTN_NARROW_H_

@@ -38,13 +38,14 @@ struct AttnArgs {
   float scale;
   int32_t type, cache_type;
   bool q_vec, o_vec;              // 16-byte loads of queries, 8-byte stores of outputs are aligned
-  int32_t rows_narrow;            // requests of at most as many rows (new tokens x query heads of a key head) take the narrow kernel, 16 or 32
-  int32_t rows_most;              // the most rows that a request of the narrow kernel can have
-  int32_t blocks_narrow;          // blocks of the narrow kernel, equal parts of all keys; 0: one for each request and key head
+  int32_t rows_narrow;            // requests of at most as many rows (new tokens x query heads of a key head) are of the narrow kind, 16 or 32; 0: none
+  int32_t rows_most;              // the most rows that a request of the narrow kind can have
+  int32_t blocks_narrow;          // blocks of the narrow kind, equal parts of all keys; 0: one for each request and key head
+  int32_t grid_narrow, grid_wide; // blocks of either kind that are launched
   int4* cuts;                     // workspace [blocks_narrow]: the pair that goes on beyond a block's part (request, key head, last block, slot), request -1: none
   float* piece; float* piece_ml;  // workspace: [blocks_narrow][2][rows_narrow][head_dim] and [..][2]
-  int32_t n_tile_wide;            // row tiles of the wide kernel at most, 0: none
-  int32_t blocks_wide;            // blocks of the wide kernel, which deal out the pairs of a row tile and a key head; 0: one for each pair
+  int32_t n_tile_wide;            // row tiles of the wide kind at most, 0: none
+  int32_t blocks_wide;            // blocks of the wide kind, which deal out the pairs of a row tile and a key head; 0: one for each pair
   int4* cuts_wide;                // workspace [blocks_wide]: the pair that goes on beyond a block's part (row tile, key head, last block, slot), row tile -1: none
   float* part; float* part_ml;    // workspace: [blocks_wide][2][rows of a tile][head_dim] and [..][2]
   WsHeader* header;

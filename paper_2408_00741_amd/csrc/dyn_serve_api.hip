@@ -201,7 +201,9 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.row_bytes = (uint32_t)row_bytes; a.page_bytes = (uint32_t)page_bytes;
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
   a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow; a.rows_most = s.rows_most;
-  a.blocks_narrow = s.blocks_narrow; a.n_tile_wide = s.n_tile_wide; a.blocks_wide = s.blocks_wide;
+  a.grid_narrow = s.rows_narrow < group ? 0 : s.blocks_narrow ? s.blocks_narrow : p->n_req * p->n_kv_head;
+  a.grid_wide = s.blocks_wide ? s.blocks_wide : s.n_tile_wide * p->n_kv_head;
+  a.blocks_narrow = a.grid_narrow ? s.blocks_narrow : 0; a.n_tile_wide = s.n_tile_wide; a.blocks_wide = s.blocks_wide;
   char* base = (char*)workspace;
   a.header = (WsHeader*)base;
   a.cuts = (int4*)(base + 256); a.piece_ml = (float*)(base + s.piece_ml); a.piece = (float*)(base + s.piece);

@@ -1,9 +1,26 @@
-// Attention over the paged cache: the launches.
-#include "dyn_attn.h"
+// Attention over the paged cache: the launches, and the kernel that joins pieces.
+#include "dyn_attn_narrow.h"
+#include "dyn_attn_wide.h"
+
+namespace {
+
+// Joins the pieces of both kinds of requests: for each block of the wide kind's parts wide::kJoinParts blocks, for each of the narrow kind's one for each row.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+  const int x = blockIdx.x, n_wide = a.blocks_wide * wide::kJoinParts;
+  if (x < n_wide) wide::join<T>(a, x / wide::kJoinParts, x % wide::kJoinParts);
+  else narrow::join<T>(a, (x - n_wide) / a.rows_most, (x - n_wide) % a.rows_most);
+}
+
+}  // namespace
 
 hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s) {
   DynTimed timed(DYN_K_ATTENTION, s);
-  hipError_t e = hipSuccess;
-  if (a.n_tile_wide > 0 && (e = dyn_launch_attend_wide(a, s)) != hipSuccess) return e;
-  return a.rows_narrow >= a.group ? dyn_launch_attend_narrow(a, s) : e;
+  if (a.grid_wide + a.grid_narrow == 0) return hipSuccess;       // no request can have a row
+  const hipError_t e = a.grid_wide > 0 ? dyn_launch_attend_mixed(a, s) : dyn_launch_attend_narrow(a, s);
+  const int joins = a.blocks_wide * wide::kJoinParts + a.blocks_narrow * a.rows_most;
+  if (e != hipSuccess || joins == 0) return e;
+  if (a.type == DYN_T_BF16) hipLaunchKernelGGL((join_kernel<__bf16>), dim3(joins), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((join_kernel<_Float16>), dim3(joins), dim3(256), 0, s, a);
+  return hipGetLastError();
 }

@@ -1,669 +1,35 @@
-// Attention for requests of many rows (new tokens x query heads of a key head): chunks of prompts.
-#include "dyn_attn.h"
+// Attention of steps with chunks: the requests of many rows, and beside them those of few.
+#include "dyn_attn_narrow.h"
+#include "dyn_attn_wide.h"
 
 namespace {
 
-__device__ __forceinline__ f32x16 mfma(x8<__bf16> a, x8<__bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mfma(x8<_Float16> a, x8<_Float16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-
-constexpr int KT = DYN_ATTN_KEYS_WIDE;
-// Of a tile of keys or values a wave carries 16 neighbouring rows from the cache to LDS, which lie in one page of 16 tokens and more.
-constexpr int kWaveRows = KT / DYN_ATTN_WAVES_WIDE;
-static_assert(kWaveRows == 16, "by_sixteen");
-
-// The value of the first lane, in a scalar register.
-__device__ __forceinline__ int32_t same(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t same(int64_t x) { return (int64_t)((uint64_t)(uint32_t)same((int32_t)(x >> 32)) << 32 | (uint32_t)same((int32_t)x)); }
-
-// Where 8 elements (16 bytes) of a tile lie in LDS, in units of 16 bytes: rows one after the other, the position in the row turned by the row so that the
-// 16 lanes of a read hit all 64 banks: 16 keys' same elements of K, 4 keys' 32 neighbouring elements of V.  (Heads of 96 have the rows of 128.)  A step of the
-// products then changes bits of the position that the key does not add to: one exclusive or makes its address.
+// One launch for both kinds of requests: the matrix instructions of the ones run beside the cache reads of the others.  Blocks go to the compute units in turn: the first 256
+// are of one kind, the next 256 of the other, so that a compute unit has one of each.
+constexpr int kTurn = DYN_ATTN_BLOCKS / 2;
 template <int DP>
-constexpr int kRow = DP <= 64 ? 8 : 16;
-template <int DP>
-__device__ __forceinline__ int k_at(int key, int c8) {
-  return DP > 64 ? key * 16 + (c8 ^ (key & 15)) : key * 8 + (c8 ^ ((key >> 1) & 7));
-}
-template <int DP>
-__device__ __forceinline__ int v_at(int key, int c8) {
-  return DP > 64 ? key * 16 + (c8 ^ ((key & 3) << 2)) : key * 8 + (c8 ^ (((key >> 1) & 1) << 2));
-}
-
-// One wave's 32 rows and what it has summed up for them.
-template <typename T, int DP>
-struct Rows {
-  x8<T> q[DP / 16];           // right operand of the first product
-  f32x16 o[DP / 32];          // O^T: column lane % 32, element 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4
-  float m, sum, c;            // reference (before c), sum of this lane's weights, log2(e) x scale x key scale
-  int32_t pos, low;           // position (-1: no row), last key that the window hides
-  int32_t first, last;        // least and greatest position in the wave
-};
-
-// Row n (of the first product's left operand) of 32 keys is key swap23(n): bits 2 and 3 swapped.
-__device__ __forceinline__ int swap23(int n) { return (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1); }
-
-// LDS by its byte address: the tiles begin at multiples of 256 bytes, so that the exclusive or of a step can be taken in the address itself.
-typedef const __attribute__((address_space(3))) u32x4* LdsRead;
-__device__ __forceinline__ uint32_t lds_address(const u32x4* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) u32x4*)p; }
-
-// S^T of a tile whose keys are in LDS.
-template <typename T, int DP>
-__device__ __forceinline__ void scores(const Rows<T, DP>& r, const u32x4* lds_k, f32x16* s) {
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-  const uint32_t at = anew(16 * k_at<DP>(swap23(lane & 31), h)) + lds_address(lds_k);      // k_at(32 mt + .., 2 d + h) is (at ^ 32 d bytes) + 32 mt rows
-#pragma unroll
-  for (int mt = 0; mt < KT / 32; ++mt) {
-    f32x16 acc = {};
-#pragma unroll
-    for (int d = 0; d < DP / 16; ++d) acc = mfma(__builtin_bit_cast(x8<T>, ((LdsRead)(uintptr_t)(at ^ 32 * d))[32 * mt * kRow<DP>]), r.q[d], acc);
-    s[mt] = acc;
-  }
-}
-
-// The rest of a tile: from the scores to the weighted sum of the values in LDS (v_at).  `key0`: the first key's position; `hidden`: some row does
-// not see all of its keys; `odd`: for each wave, whether values of the 16 rows that it carried were taken out: `marks` has two bits of each (take_out); null: none.
-template <typename T, int DP>
-__device__ __forceinline__ void weigh(const AttnArgs& a, Rows<T, DP>& r, f32x16* s, const u32x4* lds_v, bool hidden, const uint32_t* odd, const uint32_t* marks, int32_t key0) {
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-  // register i of s[mt] is key 32 mt + 16 (i / 8) + 8 h + i % 8.  What a row does not see scores -inf: weight 0 below, whatever the reference.
-  if (hidden) {
-    const int32_t mine = key0 + 8 * anew(h), from = a.window > 0 ? r.low - mine : -1, upto = r.pos - mine;      // seen: from < key <= upto, and the first tokens
-    const uint32_t width = (uint32_t)max(upto - from, 0);
-    const int32_t sinks = a.window > 0 ? min(a.n_sink - mine, upto + 1) : -1;
-#pragma unroll
-    for (int mt = 0; mt < KT / 32; ++mt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int32_t at = 32 * mt + 16 * (i / 8) + i % 8;
-        s[mt][i] = (uint32_t)(at - 1 - from) < width || at < sinks ? s[mt][i] : -INFINITY;
-        if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
-      }
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int mt = 0; mt < KT / 32; ++mt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[mt][i]);
-  top = max_across_32(top);
-  const bool raise = (top - r.m) * r.c > kRaise || (r.m == -INFINITY && top > -INFINITY);
-  if (__any(raise)) {
-    const float m = fmaxf(r.m, top);
-    const float f = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((r.m - m) * r.c);
-    r.m = m;
-    r.sum *= f;
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) r.o[t][i] *= f;
-  }
-  const float base = Kind<T>::bias - (r.m == -INFINITY ? 0.0f : r.m * r.c);
-  x8<T> p[KT / 16];
-  float sum = 0.0f;
-#pragma unroll
-  for (int mt = 0; mt < KT / 32; ++mt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], r.c, base));
-      sum += w;
-      p[2 * mt + i / 8][i % 8] = (T)w;
-    }
-  r.sum += sum;
-
-  // V^T: lane group lane / 16 has elements 16 (group % 2) + .. of keys 8 (group / 2) + ..
-  const int g16 = lane >> 4, i16 = lane & 15;
-  const uint32_t at = anew(16 * v_at<DP>(8 * (g16 >> 1) + (i16 >> 2), 2 * (g16 & 1) + ((i16 & 3) >> 1)) + 8 * (i16 & 1)) + lds_address(lds_v);      // v_at(16 st + .., 4 t + ..) is (at ^ 64 t bytes) + 16 st rows
-#pragma unroll
-  for (int st = 0; st < KT / 16; ++st)
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t) {
-      const LdsRead v = (LdsRead)(uintptr_t)(at ^ 64 * t) + 16 * st * kRow<DP>;
-      r.o[t] = mfma(__builtin_bit_cast(x8<T>, read_values(v, v + 4 * kRow<DP>)), p[st], r.o[t]);
-    }
-  // values that are not finite were taken out and marked: they go to the rows that see their keys.
-  if (odd) {
-    for (int w = 0; w < DYN_ATTN_WAVES_WIDE; ++w) {
-      if (!same((int32_t)odd[w])) continue;
-      for (int key = w * kWaveRows; key < (w + 1) * kWaveRows; ++key) {
-        const int32_t at = key0 + key;
-        const bool sees = at <= r.pos && (at > r.low || at < a.n_sink);
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t) {
-          const uint32_t up = marks[key * (DP / 32) + t] >> 4 * h, down = marks[(KT + key) * (DP / 32) + t] >> 4 * h;
-          if (!__any(up | down)) continue;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int bit = 8 * (i / 4) + i % 4;
-            r.o[t][i] += sees ? marked_value(up, down, bit) : 0.0f;
-          }
-        }
-      }
-    }
-  }
-}
-
-// Loads one wave's rows: rows base .. base + 31 of the request's `rows` for key head kvh.
-template <typename T, int DP>
-__device__ __forceinline__ void load_rows(const AttnArgs& a, const Request& q, int kvh, int32_t base, int32_t rows, Rows<T, DP>& r) {
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-  const int32_t row = base + (lane & 31);
-  const bool in = row < rows;
-  const int32_t i = (in ? row : base) / a.group, g = (in ? row : base) - i * a.group;
-  const float factor = factor_of(a, kvh);
-  r.c = size_of(factor);
-  const T* src = (const T*)a.q + (int64_t)(q.t0 + i) * a.q_token + (int64_t)(kvh * a.group + g) * a.q_head;
-  load_query<T, DP / 16>(a, src, in, factor < 0.0f ? 0x80008000u : 0u, [&](int d) { return 16 * d + 8 * h; }, r.q);
-  r.pos = in ? q.len - q.n + i : -1;
-  r.low = a.window > 0 ? r.pos - a.window : -1;
-  r.first = q.len - q.n + base / a.group;
-  r.last = q.len - q.n + (min(base + 31, rows - 1)) / a.group;
-  r.m = -INFINITY;
-  r.sum = 0.0f;
-#pragma unroll
-  for (int t = 0; t < DP / 32; ++t) r.o[t] = f32x16{};
-}
-
-// A wave's part of an 8-bit tile on its way through registers: a lane has pieces of 16 bytes, whole rows by neighbouring lanes.
-template <typename T, int DP>
-struct Stage {
-  static constexpr int kPerRow = kRow<DP> / 2, kRows = 64 / kPerRow, kEach = kWaveRows / kRows;
-  u32x4 x[kEach];
-  static __device__ __forceinline__ int first_row(int wave, int i) { return wave * kWaveRows + i * kRows; }
-  // `at`: where the wave's first row begins in the cache (by_sixteen), in bytes.  Keys beyond the request's last one are read as the last one (no row sees
-  // them), pieces beyond the head's end as its first.
-  __device__ __forceinline__ void load(const AttnArgs& a, const void* cache, int kvh, int b, int32_t key0, int32_t len, int wave, int64_t at, bool* bad) {
-    const int row_bytes = a.head_dim, lane = threadIdx.x & 63;
-    if (by_sixteen(a, key0, KT, len)) {
-      const int c = lane % kPerRow * 16;
-      const uint32_t mine = lane / kPerRow * row_bytes + (c < row_bytes ? c : 0);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) x[i] = *(const u32x4*)((const char*)cache + at + i * kRows * row_bytes + mine);
-    } else {
-      const int l = anew(lane), c = l % kPerRow * 16, off = c < row_bytes ? c : 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int32_t key = min(key0 + first_row(wave, i) + l / kPerRow, len - 1);
-        x[i] = *(const u32x4*)((const char*)cache + row_at(a, kvh, key, page_of(a, b, key, bad)) + off);
-      }
-    }
-  }
-  __device__ __forceinline__ void write_keys(const AttnArgs& a, u32x4* lds, int wave) {
-    const int lane = threadIdx.x & 63, c = lane % kPerRow;
-    if (a.head_dim < 8 * kRow<DP>) {        // beyond the head's end: zeros, as in the queries
-      const bool in = c * 16 < a.head_dim;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) x[i] = in ? x[i] : u32x4{0u, 0u, 0u, 0u};
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) lds[k_at<DP>(first_row(wave, i) + lane / kPerRow, 2 * c + e)] = widen(T{}, x[i][2 * e], x[i][2 * e + 1]);
-  }
-  __device__ __forceinline__ void write_values(u32x4* lds, bool mark, uint32_t* odd, uint8_t* marks, int wave) {
-    const int lane = threadIdx.x & 63, c = lane % kPerRow;
-    if (c >= DP / 16) return;               // heads of 96: the rest of the row is not read
-    if (mark) {
-      uint32_t bits = 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) bits |= not_finite<T>(widen(T{}, x[i][0], x[i][1])) | not_finite<T>(widen(T{}, x[i][2], x[i][3]));
-      mark = any_not_finite(bits);
-      if (lane == 0) odd[wave] = mark;
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int row = first_row(wave, i) + lane / kPerRow;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c8 = 2 * c + e;
-        u32x4 v = widen(T{}, x[i][2 * e], x[i][2 * e + 1]);
-        if (mark) v = take_out<T>(v, marks + row * (DP / 8) + c8, marks + (KT + row) * (DP / 8) + c8);
-        lds[v_at<DP>(row, c8)] = v;
-      }
-    }
-  }
-};
-
-// A wave's part of a 16-bit tile straight into LDS: no registers, no second way.  A load puts its 64 lanes' pieces one after the other, so that a lane takes the piece of its row
-// that belongs where it writes.  Pieces beyond the head's end are left out: what LDS has there is zero from the kernel's start.
-template <typename T, int DP>
-struct Direct {
-  static constexpr int kPerRow = kRow<DP>, kRows = 64 / kPerRow, kEach = kWaveRows / kRows;
-  // the piece of its row that lane `lane` takes of the wave's load i: of keys, of values (the same for all loads: their rows are multiples of 4 apart)
-  static __device__ __forceinline__ int key_piece(int i, int lane) { return k_at<DP>(i * kRows + lane / kPerRow, lane % kPerRow) % kPerRow; }
-  static __device__ __forceinline__ int value_piece(int lane) { return v_at<DP>(lane / kPerRow, lane % kPerRow) % kPerRow; }
-  template <bool KEYS>
-  static __device__ __forceinline__ void load(const AttnArgs& a, u32x4* lds, int kvh, int b, int32_t key0, int32_t len, int wave, int64_t at, bool* bad) {
-    typedef const __attribute__((address_space(1))) uint32_t* from;
-    typedef __attribute__((address_space(3))) uint32_t* to;
-    const int lane = threadIdx.x & 63, row_bytes = 2 * a.head_dim;
-    const char* cache = (const char*)(KEYS ? a.k_cache : a.v_cache);
-    u32x4* here = lds + wave * kWaveRows * kPerRow;
-    if (by_sixteen(a, key0, KT, len)) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int piece = KEYS ? key_piece(i, lane) : value_piece(lane);
-        const uint32_t mine = (i * kRows + lane / kPerRow) * row_bytes + piece * 16;
-        if (piece * 16 < row_bytes) __builtin_amdgcn_global_load_lds((from)(cache + at + mine), (to)(here + i * 64), 16, 0, 0);
-      }
-    } else {
-      const int l = anew(lane);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int piece = KEYS ? key_piece(i, l) : value_piece(l);
-        const int32_t key = min(key0 + wave * kWaveRows + i * kRows + l / kPerRow, len - 1);
-        const char* row = cache + row_at(a, kvh, key, page_of(a, b, key, bad));
-        if (piece * 16 < row_bytes) __builtin_amdgcn_global_load_lds((from)(row + piece * 16), (to)(here + i * 64), 16, 0, 0);
-      }
-    }
-  }
-  // Takes the values that are not finite out of the rows that this wave has carried, whose loads are through.
-  static __device__ __forceinline__ void mark_values(u32x4* lds, uint32_t* odd, uint8_t* marks, int wave) {
-    const int lane = anew(threadIdx.x & 63), c = value_piece(lane);
-    u32x4* mine = lds + wave * kWaveRows * kPerRow + lane;
-    uint32_t bits = 0;
-    if (c * 8 < DP)
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) bits |= not_finite<T>(mine[i * 64]);
-    const bool any = any_not_finite(bits);
-    if (lane == 0) odd[wave] = any;
-    if (!any || c * 8 >= DP) return;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int row = wave * kWaveRows + i * kRows + lane / kPerRow;
-      mine[i * 64] = take_out<T>(mine[i * 64], marks + row * (DP / 8) + c, marks + (KT + row) * (DP / 8) + c);
-    }
-  }
-};
-
-constexpr int R = 32 * DYN_ATTN_WAVES_WIDE;    // rows of a block: 32 for each wave
-
-// A row tile: R rows of a request.  Tiles are numbered so that request b's begin at cu[b] x group / R + b: the request of a tile follows from cu alone; some numbers
-// have no tile (units 0).
-struct RowTile {
-  Request q;
-  Keys keys;
-  int32_t rows, base, first, last;   // rows of the request, the tile's first row, least and greatest position in the tile
-  int32_t units;                     // tiles of keys; at least one, for rows that see nothing
-};
-__device__ __forceinline__ int64_t tiles_before(const AttnArgs& a, int b) { return (int64_t)min(max(a.cu[b], 0), a.n_token) * a.group / R + b; }
-__device__ __forceinline__ RowTile row_tile(const AttnArgs& a, int32_t tile, int b) {
-  RowTile t;
-  t.q = request_of(a, b);
-  const int64_t rows = (int64_t)t.q.n * a.group, base = ((int64_t)tile - tiles_before(a, b)) * R;
-  t.units = 0;
-  t.rows = t.base = t.first = 0;
-  t.last = -1;
-  t.keys = Keys{0, 0, 0};
-  if (rows <= a.rows_narrow || base < 0 || base >= rows) return t;
-  t.rows = (int32_t)rows;
-  t.base = (int32_t)base;
-  t.first = t.q.len - t.q.n + t.base / a.group;
-  t.last = t.q.len - t.q.n + (t.base + min(R, t.rows - t.base) - 1) / a.group;
-  if (t.last >= 0) t.keys = keys_of<KT>(a, t.first, t.last);
-  t.units = max(1, t.keys.count);
-  return t;
-}
-
-// What a block does: first some (row tile, key head) pairs as a whole, then units [at, end) of the flat range of the units of the pairs that are cut, key heads outermost.
-struct Share {
-  int32_t n_whole;               // pairs in `whole`
-  int64_t all, begin, end, at;
-  int32_t block, blocks;         // which part this is, how many there are
-  int32_t kvh, tile, unit;       // the pair at `at`, and which of its units
-  int32_t top;                   // the first tile of those that are cut; they go downwards
-};
-constexpr int kRounds = (DYN_ATTN_PAIRS_WIDE + DYN_ATTN_BLOCKS - 1) / DYN_ATTN_BLOCKS;    // whole pairs of a block at most
-struct Whole { int32_t n; int2 at[kRounds]; };   // row tile, key head
-// Deals the pairs out to a.blocks_wide blocks, which are all resident.  Where whole pairs leave blocks idle, those beyond the last full round are cut into equal parts, one for each
-// block, whose pieces join_wide_kernel joins: in four chunks over windows of 4096 keys 656 pairs of alike lengths would take two rounds of 512.  Cutting costs about kCut tiles
-// of keys (the pieces are written and read: 64 KB each): few or short pairs, and those of a prompt from its start, whose lengths even out when long ones go with short ones, stay whole.
-// Later tiles have more keys: they come first.  `lds`: two numbers for each tile.
-constexpr int32_t kCut = 20;
-__device__ __forceinline__ Share share_of(const AttnArgs& a, int32_t* lds, Whole* whole, int32_t* s_wave) {
-  constexpr int NW = DYN_ATTN_WAVES_WIDE;
-  Share s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = same(tid >> 6), G = a.n_kv_head, B = a.blocks_wide;
-  int32_t* units = lds;                       // of the tiles there are, the last tile first
-  int32_t* tiles = lds + a.n_tile_wide;       // their numbers
-  int32_t count = 0;
-  for (int32_t t0 = 0; t0 < a.n_tile_wide; t0 += 64 * NW) {
-    const int32_t t = a.n_tile_wide - 1 - (t0 + tid);
-    int32_t u = 0;
-    if (t >= 0) {
-      int lo = 0, hi = a.n_req - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tiles_before(a, mid) <= t) lo = mid; else hi = mid - 1;
-      }
-      u = row_tile(a, t, lo).units;
-    }
-    const unsigned long long there = __ballot(u > 0);
-    if (lane == 0) s_wave[wave] = __popcll(there);
-    __syncthreads();
-    int32_t at = count + __popcll(there & ((1ull << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      if (w < wave) at += s_wave[w];
-      count += s_wave[w];
-    }
-    if (u > 0) {
-      units[at] = u;
-      tiles[at] = t;
-    }
-    __syncthreads();
-  }
-  count = same(count);
-  // neighbouring parts, which read the same keys, on the same XCD: blocks go to the 8 XCDs in turn
-  s.block = B % 8 ? blockIdx.x : blockIdx.x % 8 * (B / 8) + blockIdx.x / 8;
-  // Pairs in order, heads of a tile one after the other, dealt out in rounds, every other one backwards: how long the longest share is, with all pairs and with those of full rounds
-  const int32_t pairs = count * G, rounds = pairs / B, full = rounds * B / G * G;
-  int32_t most = 0, most_full = 0;
-  for (int j = tid; j < B; j += 64 * NW) {
-    int32_t sum = 0, sum_full = 0;
-    for (int r = 0; r <= rounds; ++r) {
-      const int32_t i = r * B + (r & 1 ? B - 1 - j : j);
-      if (i >= pairs) continue;
-      sum += units[i / G];
-      if (i < full) sum_full += units[i / G];
-    }
-    most = max(most, sum);
-    most_full = max(most_full, sum_full);
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    most = max(most, __shfl_xor(most, d));
-    most_full = max(most_full, __shfl_xor(most_full, d));
-  }
-  if (lane == 0) { s_wave[wave] = most; s_wave[NW + wave] = most_full; }
-  const int32_t f = full / G, per = (count - f + 63) / 64, l0 = f + lane * per;     // tiles of full rounds; a lane's of the others
-  int64_t upto = 0;
-  for (int i = 0; i < per; ++i) upto += l0 + i < count ? units[l0 + i] : 0;
-  const int64_t mine = upto;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up(upto, d);
-    if (lane >= d) upto += o;
-  }
-  const int64_t one = same((int64_t)__shfl(upto, 63));       // units of a key head that could be cut
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    most = max(most, s_wave[w]);
-    most_full = max(most_full, s_wave[NW + w]);
-  }
-  const bool cut = same((int32_t)(most > most_full + one * G / B + kCut)) != 0;
-  if (tid == 0) {
-    int n = 0;
-    for (int r = 0; r <= rounds; ++r) {
-      const int32_t i = r * B + (r & 1 ? B - 1 - (int)blockIdx.x : (int)blockIdx.x);
-      if (i < (cut ? full : pairs)) whole->at[n++] = int2{tiles[i / G], i % G};
-    }
-    whole->n = n;
-  }
-  s.all = cut ? one * G : 0;
-  s.blocks = (int32_t)min((int64_t)B, s.all);                // each of them has a unit at least: no pair goes through a block without one
-  s.kvh = s.tile = s.unit = s.top = 0;
-  s.begin = s.end = s.at = 0;
-  if (s.block < s.blocks) {
-    s.begin = s.at = s.all * s.block / s.blocks;
-    s.end = s.all * (s.block + 1) / s.blocks;
-    s.kvh = (int32_t)(s.begin / one);
-    const int64_t in = s.begin - s.kvh * one;
-    const int l = __ffsll(__ballot(upto > in)) - 1;
-    int64_t left = in - same((int64_t)__shfl(upto - mine, l));
-    int32_t at = f + l * per;
-    while (left >= units[at]) left -= units[at++];
-    s.top = same(tiles[f]);
-    s.tile = same(tiles[at]);
-    s.unit = same((int32_t)left);
-  }
-  __syncthreads();
-  s.n_whole = same(whole->n);
-  return s;
-}
-// Where a block's pieces lie: the one at its part's begin, and the one at its end if that is another.
-__device__ __forceinline__ int64_t piece_row(int block, int slot, int row) { return ((int64_t)block * 2 + slot) * R + row; }
-
-// Requests of more rows: a block has 32 rows for each of its waves, all waves read the same tiles of 64 keys from LDS, two tiles in turn, the next
-// one's loads in flight while one is worked on.  Bound by the matrix instructions and the exponentials beside them.
+constexpr int kDimNarrow = DP <= 64 ? 64 : 128;
 template <typename T, bool F8, int DP>
-__global__ __launch_bounds__(64 * DYN_ATTN_WAVES_WIDE, 2) void attend_wide_kernel(AttnArgs a) {
-  constexpr int NW = DYN_ATTN_WAVES_WIDE, kTile = KT * kRow<DP>;   // 16-byte pieces of K (or V) of a tile
-  __shared__ __attribute__((aligned(256))) u32x4 s_tile[2][2 * kTile];
-  __shared__ uint32_t s_marks[2][2 * KT * DP / 32], s_odd[2][NW];
-  __shared__ Whole s_whole;
-  __shared__ int32_t s_wave[2 * NW];
-  static_assert(sizeof(s_tile) >= 2 * sizeof(int32_t) * DYN_ATTN_PAIRS_WIDE, "share_of");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (blockIdx.x == 0 && tid == 0) a.header->kind = DYN_WS_KIND_WORD;
-  Share sh = {};
-  if (a.blocks_wide) {
-    sh = share_of(a, (int32_t*)s_tile, &s_whole, s_wave);
-    if (tid == 0) a.cuts_wide[sh.block] = int4{-1, 0, 0, 0};
-  } else {                         // many pairs: a block is one, and the card's own order evens them out
-    sh.n_whole = 1;
-    sh.at = sh.end = 0;
+__global__ __launch_bounds__(256, 2) void attend_mixed_kernel(AttnArgs a) {
+  constexpr size_t kWide = sizeof(wide::Lds<DP>), kNarrow = sizeof(narrow::Lds<kDimNarrow<DP>, 1>);
+  __shared__ __attribute__((aligned(256))) char lds[kWide > kNarrow ? kWide : kNarrow];
+  const int x = blockIdx.x, both = min(a.grid_wide, a.grid_narrow) / kTurn * kTurn;       // of each kind that take turns
+  bool is_wide;
+  int block;
+  if (x < 2 * both) {
+    is_wide = x / kTurn % 2 == 0;
+    block = x / (2 * kTurn) * kTurn + x % kTurn;
+  } else {
+    is_wide = x - both < a.grid_wide;
+    block = is_wide ? x - both : x - a.grid_wide;
   }
-  if (!F8 && a.head_dim < DP) {    // pieces of LDS that no load writes
-    for (int i = tid; i < 4 * kTile; i += 64 * NW) (&s_tile[0][0])[i] = u32x4{0u, 0u, 0u, 0u};
-    __syncthreads();
-  }
-  bool bad = false;
-  for (int item = 0; item < sh.n_whole || sh.at < sh.end; ++item) {
-    const bool from_list = item < sh.n_whole;
-    int32_t tile = sh.tile, kvh = sh.kvh;
-    if (from_list) {
-      tile = a.blocks_wide ? same(s_whole.at[item].x) : a.n_tile_wide - 1 - (int32_t)(blockIdx.x / a.n_kv_head);
-      kvh = a.blocks_wide ? same(s_whole.at[item].y) : (int32_t)(blockIdx.x % a.n_kv_head);
-    }
-    const int b = last_request(a.n_req, [&](int b) { return tiles_before(a, b) <= tile; });
-    const RowTile rt = row_tile(a, tile, b);
-    auto next_tile = [&] {           // of those that are cut; false: there is none
-      sh.unit = 0;
-      if (--sh.tile >= 0) return true;
-      sh.tile = sh.top;
-      return ++sh.kvh < a.n_kv_head;
-    };
-    if (rt.units == 0) {             // a number without a tile
-      if (from_list || !next_tile()) break;
-      continue;
-    }
-    const Request q = rt.q;
-    const Keys keys = rt.keys;
-    const int32_t rows = rt.rows, base = rt.base, first = rt.first, last = rt.last, unit = from_list ? 0 : sh.unit;
-    const int32_t take = from_list ? rt.units : (int32_t)min((int64_t)(rt.units - unit), sh.end - sh.at);
-    const bool whole = take == rt.units;
-    const int slot = sh.at == sh.begin ? 0 : 1;
-    if (!whole && unit == 0 && tid == 0)      // the pair goes on in other blocks, the last of which has its last unit
-      a.cuts_wide[sh.block] = int4{tile, kvh, (int)(((sh.at + rt.units) * sh.blocks + sh.all - 1) / sh.all) - 1, slot};
-    const int32_t v0 = unit, v1 = min(keys.count, unit + take);
-    Rows<T, DP> r;
-    const bool idle = base + 32 * wave >= rows;
-    load_rows<T, DP>(a, q, kvh, idle ? 0 : base + 32 * wave, idle ? 0 : rows, r);
-    if (idle) r.last = -1;
-    if (v0 < v1) {
-      // where this wave's rows of the next tile begin; the table's entry is fetched a tile before
-      int64_t next = 0;
-      int32_t entry = 0;
-      auto key_at = [&](int32_t v) { return min(tile_of(keys, min(v, v1 - 1)) * KT + wave * kWaveRows, q.len - 1); };
-      auto fetch = [&](int32_t v) { entry = entry_of_all(a, b, key_at(v)); };
-      auto find = [&](int32_t v) { next = row_at(a, kvh, key_at(v), inside(a, entry, &bad)); };
-      // tiles [from, to) are seen in whole by all rows, of the block and of this wave (and others perhaps)
-      auto whole = [&](int32_t lo, int32_t hi, int32_t* from, int32_t* to) {
-        const int32_t shift = keys.first - keys.sink_tiles;              // of a tile's number and its keys, from the window on
-        *from = a.window > 0 && hi >= a.window ? max((hi - a.window) / KT + 1 - shift, keys.sink_tiles) : 0;
-        *to = max(lo + 1, 0) / KT - shift;
-        if (*to < keys.sink_tiles) *to = 0;                              // the window itself begins in the first tokens
-      };
-      int32_t block_from, block_to, wave_from, wave_to;
-      whole(first, last, &block_from, &block_to);
-      whole(r.first, r.last, &wave_from, &wave_to);
-      auto marked = [&](int32_t v) { return v < block_from || v >= block_to; };
-      // none of this wave's rows sees a key of a tile: beyond the last row's, or before the first row's window and after the first tokens
-      auto unseen = [&](int32_t key0) { return key0 > r.last || (a.window > 0 && key0 + KT - 1 <= r.first - a.window && key0 >= a.n_sink); };
-      auto work = [&](int32_t v) {
-        const u32x4* at = s_tile[(v - v0) & 1];
-        const int32_t key0 = tile_of(keys, v) * KT;
-        if (unseen(key0)) return;
-        f32x16 s[KT / 32];
-        scores<T, DP>(r, at, s);
-        weigh<T, DP>(a, r, s, at + kTile, v < wave_from || v >= wave_to, marked(v) ? s_odd[(v - v0) & 1] : nullptr, s_marks[(v - v0) & 1], key0);
-      };
-      if constexpr (!F8) {
-        using D = Direct<T, DP>;
-        auto load = [&](int32_t v) {
-          u32x4* at = s_tile[(v - v0) & 1];
-          D::template load<true>(a, at, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-          D::template load<false>(a, at + kTile, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-        };
-        fetch(v0);
-        find(v0);
-        fetch(v0 + 1);
-        load(v0);
-        for (int32_t v = v0; v < v1; ++v) {
-          __builtin_amdgcn_s_waitcnt(0x0f70);      // this wave's loads into LDS are through (vmcnt 0)
-          if (marked(v)) D::mark_values(s_tile[(v - v0) & 1] + kTile, s_odd[(v - v0) & 1], (uint8_t*)s_marks[(v - v0) & 1], wave);
-          __syncthreads();           // the tile is there, and all waves are through with the one before
-          if (v + 1 < v1) {
-            find(v + 1);
-            fetch(v + 2);
-            load(v + 1);
-          }
-          work(v);
-        }
-      } else {
-        Stage<T, DP> sk, sv;
-        auto load = [&](int32_t v) {
-          sk.load(a, a.k_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-          sv.load(a, a.v_cache, kvh, b, tile_of(keys, v) * KT, q.len, wave, next, &bad);
-        };
-        auto write = [&](int32_t v) {
-          u32x4* at = s_tile[(v - v0) & 1];
-          sk.write_keys(a, at, wave);
-          sv.write_values(at + kTile, marked(v), s_odd[(v - v0) & 1], (uint8_t*)s_marks[(v - v0) & 1], wave);
-        };
-        fetch(v0);
-        find(v0);
-        fetch(v0 + 1);
-        load(v0);
-        write(v0);
-        __syncthreads();
-        for (int32_t v = v0; v < v1; ++v) {
-          if (v + 1 < v1) {
-            find(v + 1);
-            fetch(v + 2);
-            load(v + 1);
-          }
-          work(v);
-          if (v + 1 < v1) write(v + 1);
-          __syncthreads();
-        }
-      }
-    }
-    const int32_t row = base + 32 * wave + (lane & 31);
-    const int h = lane >> 5;
-    const float sum = r.sum + __shfl_xor(r.sum, 32);
-    if (row < rows) {
-      const int32_t i = row / a.group;
-      const int head = kvh * a.group + (row - i * a.group);
-      const int64_t t = q.t0 + i;
-      const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f;
-      if (whole) {
-        const bool none = r.pos < 0;
-        const float by = vs / sum;
-#pragma unroll
-        for (int tt = 0; tt < DP / 32; ++tt)
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const int d = 32 * tt + 8 * (j / 4) + 4 * h;
-            if (d >= a.head_dim) continue;
-            float x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : r.o[tt][j + e] * by;
-            store4<T>((T*)a.out + t * a.o_token + (int64_t)head * a.o_head + d, x, a.o_vec);
-          }
-      } else {
-        const int64_t at = piece_row(sh.block, slot, row - base);
-#pragma unroll
-        for (int tt = 0; tt < DP / 32; ++tt)
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const int d = 32 * tt + 8 * (j / 4) + 4 * h;
-            if (d < a.head_dim) *(float4*)(a.part + at * a.head_dim + d) = float4{r.o[tt][j], r.o[tt][j + 1], r.o[tt][j + 2], r.o[tt][j + 3]};
-          }
-        if (h == 0) *(float2*)(a.part_ml + 2 * at) = float2{r.m, sum};
-      }
-    }
-    if (!from_list) {
-      sh.at += take;
-      if (sh.at >= sh.end || !next_tile()) break;
-    }
-    __syncthreads();               // all waves are through with the last tile of keys
-  }
-  report(a, bad);
-}
-
-// Joins the pieces of the pairs that were cut: the pair that goes on beyond attend_wide_kernel's part x.  A wave has kJoin rows, whose loads are in flight together (a row
-// a wave waited for its own: 30 us where this takes 15).  The sum goes in the order of the pieces: the same values on every run.
-constexpr int kJoin = 8;
-template <typename T>
-__global__ __launch_bounds__(256) void join_wide_kernel(AttnArgs a) {
-  const int4 cut = a.cuts_wide[blockIdx.x];
-  if (cut.x < 0) return;
-  const int lane = threadIdx.x & 63, kvh = cut.y, pieces = cut.z - blockIdx.x + 1, row0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * kJoin;
-  const int b = last_request(a.n_req, [&](int b) { return tiles_before(a, b) <= cut.x; });
-  const RowTile rt = row_tile(a, cut.x, b);
-  if (rt.base + row0 >= rt.rows) return;
-  const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f, c = size_of(factor_of(a, kvh));
-  const int at = 2 * lane;
-  const bool in = at < a.head_dim;
-  float m[kJoin], sum[kJoin];
-  float2 x[kJoin];
-#pragma unroll
-  for (int i = 0; i < kJoin; ++i) {
-    m[i] = -INFINITY;
-    sum[i] = 0.0f;
-    x[i] = float2{0.0f, 0.0f};
-  }
-  for (int p = 0; p < pieces; ++p) {
-    const int64_t from = piece_row(blockIdx.x + p, p == 0 ? cut.w : 0, row0);    // rows beyond the tile's end have room too, and are not written below
-    float2 ml[kJoin], v[kJoin];
-#pragma unroll
-    for (int i = 0; i < kJoin; ++i) {
-      ml[i] = *(const float2*)(a.part_ml + 2 * (from + i));
-      v[i] = *(const float2*)(a.part + (from + i) * a.head_dim + (in ? at : 0));
-    }
-#pragma unroll
-    for (int i = 0; i < kJoin; ++i) {
-      if (ml[i].x == -INFINITY && ml[i].y == 0.0f) continue;     // no weight in this piece
-      const float top = fmaxf(m[i], ml[i].x);
-      const float f = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml[i].x - top) * c), f0 = m[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[i] - top) * c);
-      m[i] = top;
-      sum[i] = __builtin_fmaf(ml[i].y, f, sum[i] * f0);
-      x[i].x = __builtin_fmaf(v[i].x, f, x[i].x * f0);
-      x[i].y = __builtin_fmaf(v[i].y, f, x[i].y * f0);
-    }
-  }
-  if (!in) return;
-#pragma unroll
-  for (int j = 0; j < kJoin; ++j) {
-    const int32_t row = rt.base + row0 + j;
-    if (row >= rt.rows) return;
-    const int32_t i = row / a.group;
-    const bool none = rt.q.len - rt.q.n + i < 0;
-    T* to = (T*)a.out + (int64_t)(rt.q.t0 + i) * a.o_token + (int64_t)(kvh * a.group + row - i * a.group) * a.o_head + at;
-    const float by = vs / sum[j];
-    to[0] = (T)(none ? 0.0f : x[j].x * by);
-    to[1] = (T)(none ? 0.0f : x[j].y * by);
-  }
+  if (is_wide) wide::attend<T, F8, DP>(a, block, *(wide::Lds<DP>*)lds);
+  else narrow::attend<T, F8, kDimNarrow<DP>, 1>(a, block, *(narrow::Lds<kDimNarrow<DP>, 1>*)lds);
 }
 
 template <typename T, bool F8, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  const dim3 grid(a.blocks_wide ? (unsigned)a.blocks_wide : (unsigned)a.n_tile_wide * a.n_kv_head), block(64 * DYN_ATTN_WAVES_WIDE);
-  hipLaunchKernelGGL((attend_wide_kernel<T, F8, DP>), grid, block, 0, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.blocks_wide == 0) return e;
-  hipLaunchKernelGGL((join_wide_kernel<T>), dim3((unsigned)a.blocks_wide, R / (4 * kJoin)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attend_mixed_kernel<T, F8, DP>), dim3(a.grid_wide + a.grid_narrow), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, bool F8>
@@ -675,4 +41,4 @@ hipError_t launch_type(const AttnArgs& a, hipStream_t s) { return a.cache_type =
 
 }  // namespace
 
-hipError_t dyn_launch_attend_wide(const AttnArgs& a, hipStream_t s) { return a.type == DYN_T_BF16 ? launch_type<__bf16>(a, s) : launch_type<_Float16>(a, s); }
+hipError_t dyn_launch_attend_mixed(const AttnArgs& a, hipStream_t s) { return a.type == DYN_T_BF16 ? launch_type<__bf16>(a, s) : launch_type<_Float16>(a, s); }
