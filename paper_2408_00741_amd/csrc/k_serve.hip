@@ -141,18 +141,32 @@ __device__ __forceinline__ void step_items(const KvStepArgs& a, const Ring& ring
       }
     }
   }
-  const int step = gridDim.x * kStepThreads, at = blockIdx.x * kStepThreads + tid;
-  for (int32_t e = at; e < n_need; e += step) {
-    const int b = last_at(need, 0, B - 1, e);
-    if (need[b + 1] > ring.count) continue;
-    const int32_t c = s_ctx ? s_ctx[b] : cached_of(a, b);
-    const int32_t have = (int32_t)columns_of(a, (uint32_t)c);
-    a.table[(size_t)b * a.max_pages + have + (e - need[b])] = a.ring[ring_at(a, ring, e)];
-  }
-  for (int32_t e = at; e < min(n_back, a.n_page - ring.count); e += step) {
-    const int b = last_at(back, 0, B - 1, e);
-    a.ring[ring_at(a, ring, ring.count + e)] = a.table[(size_t)b * a.max_pages + (e - back[b])];
-  }
+  // this block's part of a flat range: [first, last] of the items, [lo, hi] of their requests
+  auto part = [&](const int32_t* sums, int32_t count, int32_t* first, int32_t* last, int* lo, int* hi) {
+    const int32_t each = (int32_t)(((int64_t)count + gridDim.x - 1) / gridDim.x);
+    const int64_t from = (int64_t)blockIdx.x * each;
+    if (from >= count) return false;
+    *first = (int32_t)from;
+    *last = (int32_t)min(from + each, (int64_t)count) - 1;
+    *lo = last_at_all(sums, 0, B - 1, *first);
+    *hi = last_at_all(sums, *lo, B - 1, *last);
+    return true;
+  };
+  int32_t first, last;
+  int lo, hi;
+  if (part(need, n_need, &first, &last, &lo, &hi))
+    for (int32_t e = first + tid; e <= last; e += kStepThreads) {
+      const int b = last_at(need, lo, hi, e);
+      if (need[b + 1] > ring.count) continue;
+      const int32_t c = s_ctx ? s_ctx[b] : cached_of(a, b);
+      const int32_t have = (int32_t)columns_of(a, (uint32_t)c);
+      a.table[(size_t)b * a.max_pages + have + (e - need[b])] = a.ring[ring_at(a, ring, e)];
+    }
+  if (part(back, min(n_back, a.n_page - ring.count), &first, &last, &lo, &hi))
+    for (int32_t e = first + tid; e <= last; e += kStepThreads) {
+      const int b = last_at(back, lo, hi, e);
+      a.ring[ring_at(a, ring, ring.count + e)] = a.table[(size_t)b * a.max_pages + (e - back[b])];
+    }
 }
 
 // What is written once per request, and the free list's new state (by the block that has the sums).
@@ -293,7 +307,7 @@ hipError_t dyn_launch_kv_step(const KvStepArgs& a, hipStream_t s) {
   static_assert(DYN_KV_ONE_LAUNCH == 4 * 1024, "requests of a thread");
   if (a.n_req <= 256) hipLaunchKernelGGL((kv_step_kernel<1, 256>), grid(512), dim3(256), 0, s, a);
   else if (a.n_req <= 1024) hipLaunchKernelGGL((kv_step_kernel<4, 256>), grid(512), dim3(256), 0, s, a);
-  else if (a.n_req <= DYN_KV_ONE_LAUNCH) hipLaunchKernelGGL((kv_step_kernel<4, 1024>), grid(256), dim3(1024), 0, s, a);
+  else if (a.n_req <= DYN_KV_ONE_LAUNCH) hipLaunchKernelGGL((kv_step_kernel<4, 1024>), grid(512), dim3(1024), 0, s, a);
   else {
     hipLaunchKernelGGL(kv_sums_kernel, dim3(1), dim3(kSumThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
