@@ -1,0 +1,186 @@
+#!/usr/bin/env python3
+"""A served layer's steps over a paged key/value cache, and what they cost at a load: the measurement behind a profile's rows.
+
+A profile says what a prompt token (prefill_ms_per_tok) and a generated token (tbt_ms) cost at a load; it is measured by running steps at the
+lengths of the request classes (Section IV-A of the paper).  This runs the part of such steps that depends on those lengths: requests come with a
+prompt, which is taken in chunks beside the tokens of the requests that generate; those that are through give their pages back.  Every step is
+dyn_kv_step, dyn_rope_append and dyn_paged_attention; the layer's product is stood in for by random queries, keys and values.
+
+    python examples/serving_steps.py                     # tables of step times
+    python examples/serving_steps.py --check             # small sizes, every step against attention over each request's own keys in 64 bits
+"""
+import argparse
+import os
+import sys
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import numpy as np
+import torch
+
+import paper_2408_00741_amd as dyn
+
+
+class Layer:
+    """One layer's cache and what a server keeps beside it: block tables, the ring of free pages, lengths, a workspace."""
+
+    def __init__(self, slots, n_page, page, max_len, max_step, q_heads, kv_heads, dim, dtype=torch.bfloat16, cache=None, seed=0):
+        dev = torch.device("cuda")
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.H, self.G, self.D, self.page, self.dtype, self.max_len = q_heads, kv_heads, dim, page, dtype, max_len
+        self.k, self.v = (torch.zeros(n_page, kv_heads, page, dim, dtype=cache or dtype, device=dev) for _ in range(2))
+        self.table = torch.full((slots, -(-max_len // page)), -1, **i32)
+        self.free, self.state = torch.arange(n_page, **i32), torch.tensor([0, n_page], **i32)
+        self.ctx = torch.zeros(slots, **i32)
+        self.freq, self.amplitude = dyn.dyn_rope_frequencies(dim)
+        self.work = torch.zeros(dyn.dyn_paged_attention_workspace(slots, max_step, q_heads, kv_heads, dim, max_step, max_len), dtype=torch.uint8, device=dev)
+        self.plan_work = torch.zeros(dyn.dyn_kv_step_workspace(slots), dtype=torch.uint8, device=dev)
+        self.rng = torch.Generator(device=dev).manual_seed(seed)
+
+    def project(self, n):
+        """Stands in for the layer's product: queries, keys and values side by side."""
+        return torch.randn(n, self.H + 2 * self.G, self.D, generator=self.rng, device=self.k.device).to(self.dtype)
+
+    def step(self, new, qkv):
+        """`new`: tokens of each slot in this step (DYN_KV_RELEASE: it is through); qkv: their rows, slot after slot.  Returns the plan, the rotated
+        queries and the attention's output."""
+        n = np.maximum(new, 0)
+        p = dyn.dyn_kv_step(self.ctx, torch.from_numpy(new).cuda(), int(n.sum()), self.table, self.free, self.state, self.page, workspace=self.plan_work)
+        H, G = self.H, self.G
+        q = dyn.dyn_rope_append(qkv[:, :H], qkv[:, H:H + G], qkv[:, H + G:], p["pos"], p["slot"], self.k, self.v, self.freq, rope_scale=self.amplitude)
+        out = dyn.dyn_paged_attention(q, self.k, self.v, self.table, p["cu_new"], p["kv_len"], int(n.max()), self.max_len, workspace=self.work)
+        self.ctx, self.state = p["next_len"], p["free_state"]
+        return p, q, out
+
+    def failed(self):
+        """Status bits of the last plan and of all attention calls so far (0: none)."""
+        return dyn.dyn_workspace_status(self.plan_work) | dyn.dyn_workspace_status(self.work)
+
+
+def serve(layer, requests, slots, chunk, on_step):
+    """requests: (prompt, answer) lengths, taken in order as slots come free.  A step brings every generating request one token and the first waiting
+    prompts up to `chunk` tokens together."""
+    waiting = list(requests)
+    prompt, answer = np.zeros(slots, np.int64), np.zeros(slots, np.int64)      # tokens of each that are still to come
+    busy = np.zeros(slots, bool)
+    while waiting or busy.any():
+        new = np.zeros(slots, np.int32)
+        done = busy & (prompt + answer == 0)
+        new[done] = dyn.DYN_KV_RELEASE
+        for s in np.nonzero(~busy)[0]:
+            if waiting:
+                prompt[s], answer[s] = waiting.pop(0)
+                busy[s] = True
+        generating = busy & ~done & (prompt == 0)
+        new[generating] = 1
+        answer[generating] -= 1
+        room = chunk
+        for s in np.nonzero(busy & (prompt > 0))[0]:
+            take = min(room, int(prompt[s]))
+            new[s] = take
+            prompt[s] -= take
+            room -= take
+        busy &= ~done
+        on_step(new)
+
+
+def check(slots=6, chunk=48, seed=1):
+    """Every step of a small server against each request's keys and values kept apart."""
+    layer = Layer(slots, n_page=16 * slots, page=16, max_len=256, max_step=chunk + slots, q_heads=8, kv_heads=2, dim=64, seed=seed)
+    r = np.random.RandomState(seed)
+    requests = [(int(r.randint(1, 150)), int(r.randint(0, 20))) for _ in range(12)]
+    held = [None] * slots
+    worst, steps = 0.0, 0
+
+    def on_step(new):
+        nonlocal worst, steps
+        qkv = layer.project(int(np.maximum(new, 0).sum()))
+        if len(qkv) == 0:
+            layer.step(new, qkv)
+            held[:] = [None if n < 0 else h for n, h in zip(new, held)]
+            return
+        p, q, out = layer.step(new, qkv)
+        pos = p["pos"].double()[:, None, None] * torch.from_numpy(layer.freq).cuda()
+        k = qkv[:, layer.H:layer.H + layer.G].double()
+        a, b = k.chunk(2, -1)
+        k = torch.cat([a * pos.cos() - b * pos.sin(), b * pos.cos() + a * pos.sin()], -1).to(layer.dtype).double()
+        v, at = qkv[:, layer.H + layer.G:].double(), 0
+        for s, n in enumerate(new):
+            if n < 0:
+                held[s] = None
+            if n <= 0:
+                continue
+            rows = slice(at, at + n)
+            at += n
+            old = held[s] or (k[:0], v[:0])
+            held[s] = K, V = torch.cat([old[0], k[rows]]), torch.cat([old[1], v[rows]])
+            L = len(K)
+            seen = torch.arange(L, device="cuda") <= torch.arange(L - n, L, device="cuda")[:, None]
+            for h in range(layer.H):
+                g = h // (layer.H // layer.G)
+                w = (q[rows, h].double() @ K[:, g].T * layer.D ** -0.5).masked_fill(~seen, -float("inf")).softmax(1)
+                want, size = w @ V[:, g], w @ V[:, g].abs()
+                # one rounding of the output and one of every weight, half a step each; scores and sums in 32 bits are far below; keys differ by a
+                # rounding of their own where sine and cosine of 32 bits fall on the other side of it: a step of 2^-8 of some elements, far below u x size
+                worst = max(worst, float(((out[rows, h].double() - want).abs() / (2.0 ** -8 * (want.abs() + size) + 1e-30)).max()))
+        steps += 1
+
+    serve(layer, requests, slots, chunk, on_step)
+    assert layer.failed() == 0, layer.failed()
+    assert int(layer.state[1]) == 16 * slots, "pages were lost"
+    return worst, steps
+
+
+def timed(layer, new, repeat=20):
+    """Milliseconds of a step that leaves the lengths as they are (the next one starts from them again)."""
+    ctx, state = layer.ctx, layer.state
+    qkv = layer.project(int(np.maximum(new, 0).sum()))
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for i in range(repeat + 3):
+        if i == 3:
+            start.record()
+        layer.ctx, layer.state = ctx, state
+        layer.step(new, qkv)
+    end.record()
+    torch.cuda.synchronize()
+    layer.ctx, layer.state = ctx, state
+    return start.elapsed_time(end) / repeat
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--check", action="store_true")
+    ap.add_argument("--heads", type=int, default=64)
+    ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--dim", type=int, default=128)
+    ap.add_argument("--chunk", type=int, default=512)
+    a = ap.parse_args()
+    if a.check:
+        worst, steps = check()
+        print(f"{steps} steps: at most {worst:.2f} of the tolerance")
+        return 0 if worst <= 1.0 else 1
+    page, max_len = 16, 16384
+    print("one layer, ms a step; prompt: a chunk of %d tokens beside the requests that generate" % a.chunk)
+    print("%9s %9s %12s %14s %22s" % ("requests", "tokens", "generate", "with a prompt", "prompt ms per token"))
+    for n in (1, 8, 32, 128):
+        for length in (256, 2048, 8192):
+            pages = (n + 1) * (-(-(length + a.chunk) // page) + 1)
+            layer = Layer(n + 1, pages, page, max_len, n + a.chunk, a.heads, a.kv_heads, a.dim)
+            left = np.full(n + 1, length, np.int64)        # the cache filled through the step itself, a few thousand tokens at a time
+            while left.any():
+                new = np.minimum(left, max(1, 4096 // (n + 1))).astype(np.int32)
+                new = np.minimum(new, np.maximum(0, (n + a.chunk) - (np.cumsum(new) - new))).astype(np.int32)
+                layer.step(new, layer.project(int(new.sum())))
+                left -= new
+            one = np.ones(n + 1, np.int32)
+            one[n] = 0
+            alone = timed(layer, one)
+            one[n] = a.chunk
+            both = timed(layer, one)
+            assert layer.failed() == 0, layer.failed()
+            print("%9d %9d %12.4f %14.4f %22.6f" % (n, length, alone, both, max(both - alone, 0.0) / a.chunk))
+    return 0
+
+
+if __name__ == "__main__":
+    sys.exit(main())
