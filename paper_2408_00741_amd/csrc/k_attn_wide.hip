@@ -9,7 +9,7 @@ namespace {
 constexpr int kTurn = DYN_ATTN_BLOCKS / 2;
 template <int DP>
 constexpr int kDimNarrow = DP <= 64 ? 64 : 128;
-template <typename T, bool F8, int DP>
+template <typename T, bool F8, int DP, bool FULL>
 __global__ __launch_bounds__(256, 2) void attend_mixed_kernel(AttnArgs a) {
   constexpr size_t kWide = sizeof(wide::Lds<DP>), kNarrow = sizeof(narrow::Lds<kDimNarrow<DP>, 1>);
   __shared__ __attribute__((aligned(256))) char lds[kWide > kNarrow ? kWide : kNarrow];
@@ -23,13 +23,15 @@ __global__ __launch_bounds__(256, 2) void attend_mixed_kernel(AttnArgs a) {
     is_wide = x - both < a.grid_wide;
     block = is_wide ? x - both : x - a.grid_wide;
   }
-  if (is_wide) wide::attend<T, F8, DP>(a, block, *(wide::Lds<DP>*)lds);
+  if (is_wide) wide::attend<T, F8, DP, FULL>(a, block, *(wide::Lds<DP>*)lds);
   else narrow::attend<T, F8, kDimNarrow<DP>, 1>(a, block, *(narrow::Lds<kDimNarrow<DP>, 1>*)lds);
 }
 
 template <typename T, bool F8, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attend_mixed_kernel<T, F8, DP>), dim3(a.grid_wide + a.grid_narrow), dim3(256), 0, s, a);
+  const dim3 grid(a.grid_wide + a.grid_narrow);
+  if (!F8 && a.head_dim == DP) hipLaunchKernelGGL((attend_mixed_kernel<T, F8, DP, !F8>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_mixed_kernel<T, F8, DP, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, bool F8>
