@@ -193,7 +193,7 @@ struct Share {
   int32_t b, kvh, unit, units;   // the pair at `at`, and which of its units
 };
 // With a.blocks_narrow blocks each takes an equal part, whatever the requests' lengths are: a block's part may begin and end inside a pair, whose pieces
-// join_narrow_kernel joins.  (Pieces of a fixed length left a third of the card idle where lengths differ: 64 requests of 800 to 8192 tokens 217 us, 600 us for 96 of
+// join() puts together.  (Pieces of a fixed length left a third of the card idle where lengths differ: 64 requests of 800 to 8192 tokens 217 us, 600 us for 96 of
 // 8192, which are evenly cut.)  With 0, where the pairs are many, a block is a pair.
 __device__ __forceinline__ Share share_of(const AttnArgs& a, int block) {
   Share s;
@@ -250,9 +250,9 @@ __device__ __forceinline__ Share share_of(const AttnArgs& a, int block) {
 __device__ __forceinline__ int64_t piece_row(const AttnArgs& a, int block, int slot, int row) { return ((int64_t)block * 2 + slot) * a.rows_narrow + row; }
 
 // Requests of at most 16 NT rows.  Four waves take the tiles of a piece of a pair's keys in turn, each for all rows, and join at the piece's end.  K goes straight
-// into registers as the left operand, V through LDS; the next tile's loads are in flight while one is worked on.  Bound by the bytes of K and V: 96 requests of
-// 8192 tokens (64 heads over 8, 128 wide, 16 bits) are read at 5.7 TB/s, with the arithmetic left out at 5.7.  Two blocks a compute unit: with three registers
-// are short (5.4).
+// into registers as the left operand, V through LDS; the next tile's loads are in flight while one is worked on.  Bound by the bytes of K and V: 64 requests of 800 to
+// 8192 tokens (64 heads over 8, 128 wide, 16 bits; 877 MB) take 162 us, 5.4 TB/s, where a copy of 2 GiB moves 5.0; three of up to 131072 in 8 bits (612 MB) 112 us, 5.5.  Two blocks
+// a compute unit: with three, registers are short (a tenth slower).  One request of 1531 keys: 9.3 us, bound by the loads that wait for one another (lengths, page, keys).
 template <int DP, int NT>
 struct Lds {
   u32x4 tile[4][KT * kRow<DP>];           // a wave's values, and at the end the sums of 16 rows
@@ -441,7 +441,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP, NT>
   report(a, bad);
 }
 
-// Joins the pieces of the pairs that were cut: a block for each row of the pair that goes on beyond attend_narrow_kernel's block x.  The waves take the pieces in turn; the
+// Joins the pieces of the pairs that were cut: a block for each row of the pair that goes on beyond attend()'s block `block`.  The waves take the pieces in turn; the
 // sum goes in a fixed order: the same values on every run.  A kernel of its own: a block that waits for the others' pieces, or the last one to come, needs fences over
 // all L2s, which cost more than the launch.
 template <typename T>

@@ -193,6 +193,7 @@ __device__ __forceinline__ void write_state(const KvStepArgs& a, const Ring& r, 
 
 // Up to DYN_KV_ONE_LAUNCH requests: every block makes all sums for itself, in LDS, and takes its pieces: one launch.  What bounds a step of
 // few tokens is latency: the launch, the lengths, the sums, the table's entry, one after the other.  EACH: requests of a thread.
+// 64 requests that generate 5.5 us, 999 mixed ones (38 000 tokens) 9.2; 3000 prompts of 1.6 million tokens together 15.9 (13 MB: 2.7 us of a copy).
 template <int EACH, int kStepThreads>
 __global__ __launch_bounds__(kStepThreads) void kv_step_kernel(KvStepArgs a) {
   constexpr int kMost = EACH * kStepThreads;
@@ -364,7 +365,8 @@ __device__ __forceinline__ void put8(uint8_t* p, const float* x, float scale) {
 // (x_i, x_j) -> (x_i c - x_j s, x_j c + x_i s) for the pairs of the first `rotary` elements of every query and key head, the rest as it is; keys
 // and values into the slot's row of the cache.  A block has one token and a part of its heads; the token's angles once, in LDS: position x turns
 // per position in 64 bits, of which only the fraction of a turn counts (exact to 2^-22 of a turn at position 2^31), sine and cosine in 32.  A thread
-// has 2 V elements of a head: V pairs, or 2 V elements that are not rotated.  Bound by the bytes it moves, at few tokens by latency.
+// has 2 V elements of a head: V pairs, or 2 V elements that are not rotated.  Bound by the bytes it moves, at few tokens by latency.  4738 tokens (32 heads over
+// 8, 128 wide, an 8-bit cache; 107 MB) 20.4 us, 5.2 TB/s, where a copy of 2 GiB moves 5.0; 64 tokens 4.0 us.
 template <typename T, bool F8, int V>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   __shared__ float s_cos[DYN_ROPE_MAX_PAIRS], s_sin[DYN_ROPE_MAX_PAIRS];

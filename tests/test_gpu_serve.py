@@ -151,6 +151,29 @@ def test_attention_long_cut_in_pieces(dtype, cache, new, kv):
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))   # the same bits on every run
 
 
+@pytest.mark.parametrize("new,kv,D,G,group,window,n_sink", [
+    ([300, 1, 20, 419], [2000, 500, 1900, 2100], 16, 6, 16, 0, 0),      # 540 pairs of a row tile and a key head: full rounds of whole ones, the others cut
+    ([0, 700, 3, 40], [0, 2100, 40, 1990], 64, 3, 32, 1500, 9),         # the same under a window, with numbers that have no row tile
+    ([500], [500], 48, 8, 16, 0, 0),                                    # a prompt from its start: nothing is cut
+    ([200, 60], [260, 333], 16, 32, 32, 0, 0),                          # more pairs than are dealt out: a block is one
+    ([40, 33], [40, 333], 32, 2, 4, 0, 0)])                             # no request of few rows can be there: none is looked for
+def test_attention_row_tiles_dealt_out(new, kv, D, G, group, window, n_sink):
+    c = Cache(new, kv, G, D, 16, torch.bfloat16, seed=D)
+    q = c.queries(G * group)
+    out = c.run(q, window=window, n_sink=n_sink)
+    c.check(q, out, window=window, n_sink=n_sink)
+    assert torch.equal(out, c.run(q, window=window, n_sink=n_sink))
+
+
+def test_attention_fewer_tokens_than_rows_of_the_tensor():
+    # a captured step has room for more tokens than a step brings: one request of one token in a tensor of 64
+    c = Cache([1], [100], 2, 64, 16, torch.float16, seed=9)
+    q = torch.cat([c.queries(8), torch.zeros(63, 8, 64, dtype=torch.float16)])
+    for most in (1, 64):
+        out = c.run(q, max_new=most)
+        c.check(q[:1], out[:1])
+
+
 def test_attention_workspace_is_shared_by_calls_of_other_shapes():
     ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
     for i, (new, kv, G) in enumerate([([1, 1], [3000, 200], 1), ([90], [2500], 2), ([1] * 40, [64] * 40, 4), ([1], [5000], 1), ([200, 1], [1500, 900], 1)]):
