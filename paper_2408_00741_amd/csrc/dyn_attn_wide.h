@@ -484,7 +484,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP>& s)
     const bool whole = take == rt.units;
     const int slot = sh.at == sh.begin ? 0 : 1;
     if (!whole && unit == 0 && tid == 0)      // the pair goes on in other blocks, the last of which has its last unit
-      a.cuts_wide[sh.block] = int4{tile, kvh, (int)(((sh.at + rt.units) * sh.blocks + sh.all - 1) / sh.all) - 1, slot};
+      a.cuts_wide[sh.block] = int4{tile, kvh, 2 * ((int)(((sh.at + rt.units) * sh.blocks + sh.all - 1) / sh.all) - 1) + slot, b};
     const int32_t v0 = unit, v1 = min(keys.count, unit + take);
     Rows<T, DP> r;
     const bool idle = base + 32 * wave >= rows;
@@ -612,16 +612,15 @@ __device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP>& s)
   report(a, bad);
 }
 
-// Joins the pieces of the pairs that were cut: the pair that goes on beyond part `block`.  A wave has kJoin rows, whose loads are in flight together (with one row a wave
-// 30 us where this takes 18 for 40 MB of pieces).  The sum goes in the order of the pieces: the same values on every run.
-constexpr int kJoin = 8, kJoinParts = R / (4 * kJoin);
+// Joins the pieces of the pairs that were cut: the pair that goes on beyond part `block`.  A wave has kJoin rows and two pieces at a time, whose loads are in flight together (with
+// one row a wave 30 us for 40 MB of pieces, with eight rows and a piece at a time 22).  The sum goes in the order of the pieces: the same values on every run.
+constexpr int kJoin = 4, kJoinParts = R / (4 * kJoin);
 template <typename T>
 __device__ __forceinline__ void join(const AttnArgs& a, int block, int part) {
   const int4 cut = a.cuts_wide[block];
   if (cut.x < 0) return;
-  const int lane = threadIdx.x & 63, kvh = cut.y, pieces = cut.z - block + 1, row0 = (part * 4 + (threadIdx.x >> 6)) * kJoin;
-  const int b = last_request(a.n_req, [&](int b) { return tiles_before(a, b) <= cut.x; });
-  const RowTile rt = row_tile(a, cut.x, b);
+  const int lane = threadIdx.x & 63, kvh = cut.y, pieces = cut.z / 2 - block + 1, row0 = (part * 4 + (threadIdx.x >> 6)) * kJoin;
+  const RowTile rt = row_tile(a, cut.x, cut.w);
   if (rt.base + row0 >= rt.rows) return;
   const float vs = a.v_scale ? a.v_scale[kvh] : 1.0f, c = size_of(factor_of(a, kvh));
   const int at = 2 * lane;
@@ -634,24 +633,31 @@ __device__ __forceinline__ void join(const AttnArgs& a, int block, int part) {
     sum[i] = 0.0f;
     x[i] = float2{0.0f, 0.0f};
   }
-  for (int p = 0; p < pieces; ++p) {
-    const int64_t from = piece_row(block + p, p == 0 ? cut.w : 0, row0);    // rows beyond the tile's end have room too, and are not written below
-    float2 ml[kJoin], v[kJoin];
+  for (int p0 = 0; p0 < pieces; p0 += 2) {
+    float2 ml[2][kJoin], v[2][kJoin];
 #pragma unroll
-    for (int i = 0; i < kJoin; ++i) {
-      ml[i] = *(const float2*)(a.part_ml + 2 * (from + i));
-      v[i] = *(const float2*)(a.part + (from + i) * a.head_dim + (in ? at : 0));
+    for (int k = 0; k < 2; ++k) {
+      const int p = min(p0 + k, pieces - 1);
+      const int64_t from = piece_row(block + p, p == 0 ? cut.z % 2 : 0, row0);    // rows beyond the tile's end have room too, and are not written below
+#pragma unroll
+      for (int i = 0; i < kJoin; ++i) {
+        ml[k][i] = *(const float2*)(a.part_ml + 2 * (from + i));
+        v[k][i] = *(const float2*)(a.part + (from + i) * a.head_dim + (in ? at : 0));
+      }
     }
 #pragma unroll
-    for (int i = 0; i < kJoin; ++i) {
-      if (ml[i].x == -INFINITY && ml[i].y == 0.0f) continue;     // no weight in this piece
-      const float top = fmaxf(m[i], ml[i].x);
-      const float f = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml[i].x - top) * c), f0 = m[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[i] - top) * c);
-      m[i] = top;
-      sum[i] = __builtin_fmaf(ml[i].y, f, sum[i] * f0);
-      x[i].x = __builtin_fmaf(v[i].x, f, x[i].x * f0);
-      x[i].y = __builtin_fmaf(v[i].y, f, x[i].y * f0);
-    }
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < kJoin; ++i) {
+        const float2 w = ml[k][i];
+        if (p0 + k >= pieces || (w.x == -INFINITY && w.y == 0.0f)) continue;     // no piece, no weight in it
+        const float top = fmaxf(m[i], w.x);
+        const float f = w.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((w.x - top) * c), f0 = m[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[i] - top) * c);
+        m[i] = top;
+        sum[i] = __builtin_fmaf(w.y, f, sum[i] * f0);
+        x[i].x = __builtin_fmaf(v[k][i].x, f, x[i].x * f0);
+        x[i].y = __builtin_fmaf(v[k][i].y, f, x[i].y * f0);
+      }
   }
   if (!in) return;
 #pragma unroll

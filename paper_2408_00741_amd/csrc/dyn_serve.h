@@ -46,7 +46,7 @@ struct AttnArgs {
   float* piece; float* piece_ml;  // workspace: [blocks_narrow][2][rows_narrow][head_dim] and [..][2]
   int32_t n_tile_wide;            // row tiles of the wide kind at most, 0: none
   int32_t blocks_wide;            // blocks of the wide kind, which deal out the pairs of a row tile and a key head; 0: one for each pair
-  int4* cuts_wide;                // workspace [blocks_wide]: the pair that goes on beyond a block's part (row tile, key head, last block, slot), row tile -1: none
+  int4* cuts_wide;                // workspace [blocks_wide]: the pair that goes on beyond a block's part (row tile, key head, 2 x last block + slot, request), row tile -1: none
   float* part; float* part_ml;    // workspace: [blocks_wide][2][rows of a tile][head_dim] and [..][2]
   WsHeader* header;
 };
