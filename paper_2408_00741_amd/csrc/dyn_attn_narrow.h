@@ -441,68 +441,71 @@ __device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP, NT>
   report(a, bad);
 }
 
-// Joins the pieces of the pairs that were cut: a block for each row of the pair that goes on beyond attend()'s block `block`.  The waves take the pieces in turn; the
+// Joins the pieces of the pairs that were cut: the pair that goes on beyond attend()'s block `block`, every a.join_rows-th row of it from `part`.  The waves take the pieces in turn; the
 // sum goes in a fixed order: the same values on every run.  A kernel of its own: a block that waits for the others' pieces, or the last one to come, needs fences over
 // all L2s, which cost more than the launch.
 template <typename T>
-__device__ __forceinline__ void join(const AttnArgs& a, int block, int row) {
+__device__ __forceinline__ void join(const AttnArgs& a, int block, int part) {
   __shared__ float s_m[4], s_sum[4];
   __shared__ float2 s_x[4][64];
   const int4 cut = a.cuts[block];
   if (cut.x < 0) return;
   const int b = cut.x, kvh = cut.y, pieces = cut.z - block + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Request q = request_of(a, b);
-  if (row >= q.n * a.group) return;
   const float c = size_of(factor_of(a, kvh));
   const bool in = 2 * lane < a.head_dim;
-  float m = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
-  for (int p0 = wave; p0 < pieces; p0 += 32) {
-    float2 ml[8], v[8];
-    float top = m;
+  for (int row = part; row < q.n * a.group; row += a.join_rows) {
+    float m = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
+    for (int p0 = wave; p0 < pieces; p0 += 32) {
+      float2 ml[8], v[8];
+      float top = m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int p = min(p0 + 4 * i, pieces - 1);
-      const int64_t at = piece_row(a, block + p, p == 0 ? cut.w : 0, row);
-      ml[i] = *(const float2*)(a.piece_ml + 2 * at);
-      v[i] = *(const float2*)(a.piece + at * a.head_dim + (in ? 2 * lane : 0));
+      for (int i = 0; i < 8; ++i) {
+        const int p = min(p0 + 4 * i, pieces - 1);
+        const int64_t at = piece_row(a, block + p, p == 0 ? cut.w : 0, row);
+        ml[i] = *(const float2*)(a.piece_ml + 2 * at);
+        v[i] = *(const float2*)(a.piece + at * a.head_dim + (in ? 2 * lane : 0));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+      const float f0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * c);
+      sum *= f0;
+      x *= f0;
+      y *= f0;
+      m = top;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (p0 + 4 * i >= pieces || (ml[i].x == -INFINITY && ml[i].y == 0.0f)) continue;     // no weight in this piece
+        const float f = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
+        sum = __builtin_fmaf(ml[i].y, f, sum);
+        x = __builtin_fmaf(v[i].x, f, x);
+        y = __builtin_fmaf(v[i].y, f, y);
+      }
     }
+    if (lane == 0) { s_m[wave] = m; s_sum[wave] = sum; }
+    s_x[wave][lane] = float2{x, y};
+    __syncthreads();
+    if (wave == 0 && in) {
+      const float all = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+      sum = x = y = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
-    const float f0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * c);
-    sum *= f0;
-    x *= f0;
-    y *= f0;
-    m = top;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (p0 + 4 * i >= pieces || (ml[i].x == -INFINITY && ml[i].y == 0.0f)) continue;     // no weight in this piece
-      const float f = ml[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
-      sum = __builtin_fmaf(ml[i].y, f, sum);
-      x = __builtin_fmaf(v[i].x, f, x);
-      y = __builtin_fmaf(v[i].y, f, y);
+      for (int w = 0; w < 4; ++w) {
+        if (s_m[w] == -INFINITY && s_sum[w] == 0.0f) continue;
+        const float f = s_m[w] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s_m[w] - all) * c);
+        sum = __builtin_fmaf(s_sum[w], f, sum);
+        x = __builtin_fmaf(s_x[w][lane].x, f, x);
+        y = __builtin_fmaf(s_x[w][lane].y, f, y);
+      }
+      const int32_t i = row / a.group;
+      const int64_t t = q.t0 + i;
+      const bool none = q.len - q.n + i < 0;
+      const float by = (a.v_scale ? a.v_scale[kvh] : 1.0f) / sum;
+      T* to = (T*)a.out + t * a.o_token + (int64_t)(kvh * a.group + row - i * a.group) * a.o_head + 2 * lane;
+      to[0] = (T)(none ? 0.0f : x * by);
+      to[1] = (T)(none ? 0.0f : y * by);
     }
+    __syncthreads();
   }
-  if (lane == 0) { s_m[wave] = m; s_sum[wave] = sum; }
-  s_x[wave][lane] = float2{x, y};
-  __syncthreads();
-  if (wave != 0 || !in) return;
-  const float all = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  sum = x = y = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (s_m[w] == -INFINITY && s_sum[w] == 0.0f) continue;
-    const float f = s_m[w] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s_m[w] - all) * c);
-    sum = __builtin_fmaf(s_sum[w], f, sum);
-    x = __builtin_fmaf(s_x[w][lane].x, f, x);
-    y = __builtin_fmaf(s_x[w][lane].y, f, y);
-  }
-  const int32_t i = row / a.group;
-  const int64_t t = q.t0 + i;
-  const bool none = q.len - q.n + i < 0;
-  const float by = (a.v_scale ? a.v_scale[kvh] : 1.0f) / sum;
-  T* to = (T*)a.out + t * a.o_token + (int64_t)(kvh * a.group + row - i * a.group) * a.o_head + 2 * lane;
-  to[0] = (T)(none ? 0.0f : x * by);
-  to[1] = (T)(none ? 0.0f : y * by);
 }
 
 }  // namespace narrow

@@ -613,7 +613,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, int block, Lds<DP>& s)
 }
 
 // Joins the pieces of the pairs that were cut: the pair that goes on beyond part `block`.  A wave has kJoin rows and two pieces at a time, whose loads are in flight together (with
-// one row a wave 30 us for 40 MB of pieces, with eight rows and a piece at a time 22).  The sum goes in the order of the pieces: the same values on every run.
+// one row a wave 30 us for 40 MB of pieces, with eight rows and a piece at a time 20, with these 15).  The sum goes in the order of the pieces: the same values on every run.
 constexpr int kJoin = 4, kJoinParts = R / (4 * kJoin);
 template <typename T>
 __device__ __forceinline__ void join(const AttnArgs& a, int block, int part) {

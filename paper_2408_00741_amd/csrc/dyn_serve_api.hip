@@ -202,6 +202,8 @@ int dyn_paged_attention(const dyn_attention* p, void* workspace, size_t workspac
   a.scale = p->scale; a.type = p->type; a.cache_type = p->cache_type;
   a.q_vec = aligned_rows(p->q, 8); a.o_vec = aligned_rows(p->out, 4); a.rows_narrow = s.rows_narrow; a.rows_most = s.rows_most;
   a.grid_narrow = s.rows_narrow < group ? 0 : s.blocks_narrow ? s.blocks_narrow : p->n_req * p->n_kv_head;
+  // beside chunks rows_most is what a request could have, not what single tokens do: blocks without a row cost more than a second row
+  a.join_rows = s.n_tile_wide ? std::min(s.rows_most, 4) : s.rows_most;
   a.grid_wide = s.blocks_wide ? s.blocks_wide : s.n_tile_wide * p->n_kv_head;
   a.blocks_narrow = a.grid_narrow ? s.blocks_narrow : 0; a.n_tile_wide = s.n_tile_wide; a.blocks_wide = s.blocks_wide;
   char* base = (char*)workspace;

@@ -4,12 +4,12 @@
 
 namespace {
 
-// Joins the pieces of both kinds of requests: for each block of the wide kind's parts wide::kJoinParts blocks, for each of the narrow kind's one for each row.
+// Joins the pieces of both kinds of requests: for each block of the wide kind's parts wide::kJoinParts blocks, for each of the narrow kind's a.join_rows.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int x = blockIdx.x, n_wide = a.blocks_wide * wide::kJoinParts;
   if (x < n_wide) wide::join<T>(a, x / wide::kJoinParts, x % wide::kJoinParts);
-  else narrow::join<T>(a, (x - n_wide) / a.rows_most, (x - n_wide) % a.rows_most);
+  else narrow::join<T>(a, (x - n_wide) / a.join_rows, (x - n_wide) % a.join_rows);
 }
 
 }  // namespace
@@ -18,7 +18,7 @@ hipError_t dyn_launch_paged_attention(const AttnArgs& a, hipStream_t s) {
   DynTimed timed(DYN_K_ATTENTION, s);
   if (a.grid_wide + a.grid_narrow == 0) return hipSuccess;       // no request can have a row
   const hipError_t e = a.grid_wide > 0 ? dyn_launch_attend_mixed(a, s) : dyn_launch_attend_narrow(a, s);
-  const int joins = a.blocks_wide * wide::kJoinParts + a.blocks_narrow * a.rows_most;
+  const int joins = a.blocks_wide * wide::kJoinParts + a.blocks_narrow * a.join_rows;
   if (e != hipSuccess || joins == 0) return e;
   if (a.type == DYN_T_BF16) hipLaunchKernelGGL((join_kernel<__bf16>), dim3(joins), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((join_kernel<_Float16>), dim3(joins), dim3(256), 0, s, a);
